@@ -397,6 +397,62 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
                           float* lse_dev, int32_t* status_dev, void* stream);
 
 /*
+ * The window of recent tokens as pages, and positions.  Section 5.3 keeps generated tokens unquantised; a serving engine keeps
+ * them behind a block table like the packed cache, and rotary position embedding turns queries and keys on their way in.
+ *
+ * The pool: [n_pages][n_kv_heads][K | V][page_tokens][head_dim] elements of one dtype (pq_window_bytes), contiguous, so the
+ * rows of a page can be read as they are (e.g. to be encoded into the packed cache later).  pq_paging as above, but
+ * page_tokens is any multiple of 16; token w of sequence b's window is row w % page_tokens of physical page
+ * page_table[b * pages_per_seq + w / page_tokens].  window_lens_dev, int32[batch]: tokens in each window.
+ *
+ * pq_rotary_frequencies (host): frequencies_host[i] = theta^(-2 i / rotary_dim), i < rotary_dim / 2 (rotary_dim even).  Any
+ * other frequencies (scaled ones, say) can be used in their place.
+ *
+ * pq_append_window: for every new row i of sequence b, w = window_lens[b] + (i - cu_seqlens[b]), position p = offsets[b] + w:
+ * the pairs (x, y) of the first rotary_dim elements of every query and key head become (x cos a - y sin a, y cos a + x sin a)
+ * with a = p * frequencies[pair]; the other elements, and values, are copied.  Keys and values go to row w of the window,
+ * queries to q_out, and window_lens[b] grows by the sequence's row count.
+ *   q_dev, k_dev, v_dev  [total_tokens][heads][head_dim] elements of `dtype`; element (t, h, i) of q is at t*q_token_stride +
+ *                      h*q_head_stride + i, of k and v at t*kv_token_stride + h*kv_head_stride + i (strides in elements; the
+ *                      three may be parts of one projection's rows).  q_dev = NULL: no queries (n_q_heads = 0, q_out = NULL).
+ *                      Unlike other device pointers these three, and q_out, need only their element's alignment
+ *   q_out_dev          [total_tokens][n_q_heads][head_dim] contiguous; may be q_dev where q is laid out so
+ *   cu_seqlens_dev     int32[batch+1] as for pq_encode_kv, but rows behind cu[batch] are allowed and left alone (a padded
+ *                      batch: neither read nor written); NULL: row b is sequence b's (total_tokens = batch)
+ *   frequencies_dev    float64[rotary_dim / 2], NULL with rotary_dim = 0 (no rotation).  Like S_dev it is read during set-up
+ *   interleaved        0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1)
+ *   offsets_dev        int32[batch], position of each window's first token (the lengths of a packed cache, say); NULL: 0
+ * The angle is formed in float64 and reduced to a turn before its cosine and sine are taken in float32; products and sums are
+ * float32, rounded once.  A sequence that would exceed pages_per_seq * page_tokens keeps its window and records
+ * PQ_ERR_CAPACITY; a row whose page lies outside the pool is not written, its sequence does not grow, and PQ_ERR_INVALID_ARG
+ * is recorded, as it is where cu[b+1] exceeds total_tokens.  The queries of such sequences are rotated all the same.
+ *
+ * pq_window_attention: attention (Eq. 2) of the last n_q positions of every sequence over its window: query j sees the tokens
+ * t < window_lens[b] - (n_q - 1 - j), as in pq_multi_query_attention.  Scores, softmax and sums are float32.
+ *   q_dev, out_dev     [batch][n_q][n_q_heads][head_dim] of io_dtype; kv_dtype: the pool's (either of the two)
+ *   max_len            host-side upper bound on window_lens[b] (used only to cut the work)
+ *   lse_dev            float32 [batch][n_q][n_q_heads] or NULL.  A query that sees no token, or only scores of -inf, yields
+ *                      zeros; without lse_dev the former records PQ_ERR_EMPTY, with it lse = -inf says so
+ *   workspace_dev      pq_window_workspace_bytes(...) bytes; need not be initialised; two calls that overlap in time must not
+ *                      share it
+ * head_dim is 16, 32, 64 or 128 (of the window), batch at most 65535.  What rows past a window's end hold does not matter.
+ */
+int32_t pq_rotary_frequencies(int32_t rotary_dim, double theta, double* frequencies_host);
+int64_t pq_window_bytes(int32_t head_dim, int32_t n_kv_heads, int32_t page_tokens, int32_t n_pages, int32_t dtype);
+int32_t pq_append_window(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, const void* k_dev,
+                         const void* v_dev, int32_t dtype, int64_t q_token_stride, int64_t q_head_stride,
+                         int64_t kv_token_stride, int64_t kv_head_stride, const int32_t* cu_seqlens_dev, int32_t batch,
+                         int32_t total_tokens, const double* frequencies_dev, int32_t rotary_dim, int32_t interleaved,
+                         const int32_t* offsets_dev, void* q_out_dev, void* pool_dev, int32_t* window_lens_dev,
+                         const pq_paging* paging, int32_t* status_dev, void* stream);
+int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t max_len);
+int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
+                            const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
+                            const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
+                            void* workspace_dev, int32_t* status_dev, void* stream);
+
+/*
  * General recursion depth and bit tables.  Definition 1 recurses log2 d times and Section 4 counts
  * b_FPN + (d - 1) b bits per vector for b bits per angle; Section 4.1 stops at L = 4 with (4,2,2,2) bits, which the
  * entry points above implement at speed.  The pq_general_* entry points take any head_dim = 2^k <= 256, any

@@ -67,6 +67,14 @@ _SIGNATURES = {
                                      c_void_p, c_void_p, c_void_p]),
     "pq_tail_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_void_p,
                                     c_int32, c_int32, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "pq_rotary_frequencies": (c_int32, [c_int32, c_double, c_void_p]),
+    "pq_window_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "pq_append_window": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int64, c_int64, c_int64, c_int64,
+                                   c_void_p, c_int32, c_int32, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p, c_void_p, c_void_p]),
+    "pq_window_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "pq_window_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_int32,
+                                      c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "pq_general_sizes": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "pq_general_fit_codebooks": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "pq_general_cache_bytes": (c_int64, [c_void_p, c_int32, c_int32, c_int32]),
@@ -166,6 +174,28 @@ def _torch_stream(stream, device):
     if stream is None or isinstance(stream, torch.cuda.Stream):
         return stream
     return torch.cuda.ExternalStream(stream.cuda_stream, device=device)
+
+
+def _on(stream, device):
+    """Makes `stream` the one that new tensors belong to (None: the current one)."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, device))
+
+
+def _stream_workspace(kept: dict, need: int, stream, device):
+    """At least `need` bytes that belong to `stream` (None: the device's current one): calls on different streams may overlap, so each
+    has its own.  A capture has one too, from the graph's pool: calls outside must not share it with a replay."""
+    if stream is None and device.type == "cuda":
+        stream = torch.cuda.current_stream(device)
+    key = (stream.cuda_stream, torch.cuda.is_current_stream_capturing())
+    ws = kept.get(key)
+    if ws is None or ws.numel() < need or key[1]:
+        while len(kept) >= 8 and key not in kept:   # of streams that are no longer used
+            kept.pop(next(iter(kept)))
+        with _on(stream, device):
+            ws = torch.empty(need, dtype=torch.uint8, device=device)
+        if not key[1]:
+            kept[key] = ws
+    return ws
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -349,6 +379,39 @@ def sharded_decode_attention(cache, q, dist, group=None, scale=None, stream=None
     out32, lse = cache.attend_lse(q.float(), scale=scale, stream=stream)
     parts_out, parts_lse = gather_partials(out32, lse, dist, group)
     return pq_merge_attention(parts_out, parts_lse, torch.empty_like(q), cache.status, stream=stream)
+
+
+def pq_rotary_frequencies(rotary_dim: int, theta: float = 10000.0) -> torch.Tensor:
+    """theta^(-2 i / rotary_dim) for i < rotary_dim / 2 (float64 CPU tensor): radians per position."""
+    out = torch.empty(max(rotary_dim, 0) // 2, dtype=torch.float64)
+    _check(lib().pq_rotary_frequencies(rotary_dim, theta, out.data_ptr()), "pq_rotary_frequencies")
+    return out
+
+
+def pq_window_bytes(d: int, n_kv_heads: int, page_tokens: int, n_pages: int, dtype=torch.bfloat16) -> int:
+    n = int(lib().pq_window_bytes(d, n_kv_heads, page_tokens, n_pages, _dtype_code(torch.empty(0, dtype=dtype))))
+    if n < 0:
+        raise PolarQuantError(n, "pq_window_bytes")
+    return n
+
+
+def pq_append_window(q, k, v, cu_seqlens, frequencies, interleaved, offsets, q_out, pool, lens, status, paging, stream=None):
+    """Rotate the new rows of q [total, Hq, d] and k [total, Hkv, d] by their positions, put k and v into the paged window
+    (pool [pages, Hkv, 2, page_tokens, d]; paging: (page table, tokens per page, pages)) and the queries into q_out; lens advances."""
+    _check((_native or native()).append_window(q, k, v, cu_seqlens, frequencies, interleaved, offsets, q_out, pool, lens, status, paging, stream),
+           "pq_append_window")
+
+
+def pq_window_workspace_bytes(d: int, batch: int, n_q: int, n_q_heads: int, n_kv_heads: int, max_len: int) -> int:
+    n = int(lib().pq_window_workspace_bytes(d, batch, n_q, n_q_heads, n_kv_heads, max_len))
+    if n < 0:
+        raise PolarQuantError(n, "pq_window_workspace_bytes")
+    return n
+
+
+def pq_window_attention(q, pool, lens, max_len, scale, out, lse, workspace, status, paging, stream=None):
+    """Exact attention of the last positions of every sequence, q [B, Hq, d] or [B, n_q, Hq, d], over its paged window."""
+    _check((_native or native()).window_attend(q, pool, lens, max_len, scale, out, lse, workspace, status, paging, stream), "pq_window_attention")
 
 
 def pq_paged_cache_bytes(d: int, n_kv_heads: int, page_tokens: int, n_pages: int) -> int:
@@ -545,6 +608,63 @@ class PagedPolarQuantCache(PolarQuantCache):
                                          self.batch, ctypes.addressof(pg), n_tokens, _ptr(out), _stream(None)),
                "pq_dequant_kv_paged")
         return out
+
+
+class PagedWindow:
+    """The uncompressed window of recent tokens behind a block table: pool [n_pages, Hkv, 2, page_tokens, d] (index 2: 0 = K,
+    1 = V), page_table int32 [batch, pages_per_seq].  `frequencies`: float64 [rotary_dim / 2] radians per position
+    (pq_rotary_frequencies), applied to the queries and keys of `append`; None: rows come rotated, or have no positions."""
+
+    def __init__(self, batch, n_q_heads, n_kv_heads, d, page_tokens, n_pages, page_table, dtype=torch.bfloat16, frequencies=None,
+                 interleaved=False, device="cuda"):
+        pq_window_bytes(d, n_kv_heads, page_tokens, n_pages, dtype)   # refuses what the kernels do not take
+        self.batch, self.n_q_heads, self.n_kv_heads, self.d = batch, n_q_heads, n_kv_heads, d
+        self.page_tokens, self.n_pages, self.interleaved = page_tokens, n_pages, bool(interleaved)
+        self.device = torch.device(device)
+        self.page_table = page_table.to(torch.int32).to(self.device).contiguous()
+        assert self.page_table.dim() == 2 and self.page_table.shape[0] == batch
+        self.capacity = page_tokens * self.page_table.shape[1]
+        self.frequencies = None if frequencies is None else frequencies.to(torch.float64).to(self.device).contiguous()
+        self.pool = torch.empty((n_pages, n_kv_heads, 2, page_tokens, d), dtype=dtype, device=self.device)
+        self.lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
+        self.status = torch.zeros(STATUS_WORDS, dtype=torch.int32, device=self.device)
+        self._ws, self._need = {}, {}   # workspaces by stream, bytes by (queries, max_len)
+
+    def _paging_args(self):
+        return self.page_table, self.page_tokens, self.n_pages
+
+    def append(self, q, k, v, cu_seqlens=None, offsets=None, q_out=None, stream=None):
+        """New rows of every sequence: q [total, Hq, d] (or None), k, v [total, Hkv, d], of which cu_seqlens[b] .. cu_seqlens[b + 1] - 1
+        are sequence b's (None: one each); token w of the window has position offsets[b] + w.  Returns the rotated queries."""
+        if q is not None and q_out is None:
+            with _on(stream, self.device):
+                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        pq_append_window(q, k, v, cu_seqlens, self.frequencies, self.interleaved, offsets, q_out, self.pool, self.lens, self.status,
+                         self._paging_args(), stream)
+        return q_out
+
+    def _workspace(self, n_q, max_len, stream):
+        need = self._need.get((n_q, max_len))
+        if need is None:
+            need = self._need[n_q, max_len] = pq_window_workspace_bytes(self.d, self.batch, n_q, self.n_q_heads, self.n_kv_heads, max_len)
+        return _stream_workspace(self._ws, need, stream, self.device)
+
+    def attend(self, q, out=None, scale=None, max_len=None, lse=None, stream=None):
+        """q [B, Hq, d], or [B, n_q, Hq, d] for the last n_q positions of every window (causal).  max_len: a bound on the lengths.
+        lse: float32 [B, (n_q,) Hq] to write the log-sum-exps to."""
+        if out is None:
+            with _on(stream, self.device):
+                out = torch.empty_like(q)
+        most = self.capacity if max_len is None else max_len
+        pq_window_attention(q, self.pool, self.lens, most, self.d ** -0.5 if scale is None else scale, out, lse,
+                            self._workspace(q.shape[1] if q.dim() == 4 else 1, most, stream), self.status, self._paging_args(), stream)
+        return out
+
+    def check_status(self):
+        st = self.status.cpu().tolist()
+        if st[0] != OK:
+            raise PolarQuantError(st[0], "device status")
+        return st
 
 
 class GeneralConfig(ctypes.Structure):

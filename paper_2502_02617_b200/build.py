@@ -10,7 +10,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpolarquant.so")
 BINDING = os.path.join(HERE, "_pq_binding.so")
-SOURCES = ["pq_host.cu", "pq_encode.cu", "pq_decode.cu", "pq_general.cu"]
+SOURCES = ["pq_host.cu", "pq_encode.cu", "pq_decode.cu", "pq_general.cu", "pq_window.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]
 HEADER = os.path.join(HERE, "..", "include", "polarquant.h")

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -275,7 +276,98 @@ PyObject* merge(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// The device that all tensors of a call lie on.
+c10::Device one_device(std::initializer_list<const at::Tensor*> tensors) {
+  const at::Tensor* first = *tensors.begin();
+  check(first->is_cuda(), "tensors on a CUDA device are taken");
+  for (const at::Tensor* t : tensors) check(t == nullptr || t->device() == first->device(), "all tensors must be on one device");
+  return first->device();
+}
+// Makes the tensors' device the current one for a call, whichever is current outside.
+void* stream_on(const c10::Device& device, PyObject* o) {
+  return o == Py_None ? c10::cuda::getCurrentCUDAStream(device.index()).stream() : stream_of(o);
+}
+const at::Tensor& int32s(PyObject* o, int64_t n, const char* text) {
+  const at::Tensor& t = tensor(o);
+  check(t.scalar_type() == at::kInt && t.is_contiguous() && t.numel() == n, text);
+  return t;
+}
+// A pool of pages [page][kv head][K | V][token][head_dim] and the table behind `paging`.
+struct PoolArg {
+  const at::Tensor& pool;
+  const PagingArg paging;
+  PoolArg(PyObject* p, PyObject* pg, int64_t batch, int64_t d) : pool(tensor(p)), paging(pg) {
+    check(PyTuple_Check(pg), "paging is (page table, tokens per page, pages)");
+    const at::Tensor& table = tensor(PyTuple_GET_ITEM(pg, 0));
+    check(pool.dim() == 5 && pool.is_contiguous() && pool.size(0) == paging.get()->n_pages && pool.size(2) == 2 &&
+              pool.size(3) == paging.get()->page_tokens && pool.size(4) == d,
+          "the pool must be a contiguous tensor [pages, kv heads, 2, tokens per page, head_dim]");
+    check(table.size(0) == batch && table.device() == pool.device(), "the page table must name the pages of every sequence, on the pool's device");
+  }
+};
+
+// append_window(q or None, k, v, cu_seqlens or None, frequencies or None, interleaved, offsets or None, q_out or None, pool, lens, status, paging,
+//               stream)
+PyObject* append_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 13, [&]() -> int32_t {
+    const at::Tensor *q = tensor_or_none(a[0]), *freq = tensor_or_none(a[4]), *q_out = tensor_or_none(a[7]);
+    const at::Tensor &k = tensor(a[1]), &v = tensor(a[2]), &lens = tensor(a[9]), &status = tensor(a[10]);
+    check_rows(k, v);
+    check(lens.scalar_type() == at::kInt && lens.is_contiguous() && lens.dim() == 1, "lens must be a contiguous int32 tensor [batch]");
+    const int64_t batch = lens.size(0), total = k.size(0), d = k.size(2);
+    const PoolArg pool(a[8], a[11], batch, d);
+    check(pool.pool.scalar_type() == k.scalar_type() && pool.pool.size(1) == k.size(1), "k and v must have the pool's dtype and kv heads");
+    check((q == nullptr) == (q_out == nullptr), "q and q_out go together");
+    if (q != nullptr)
+      check(q->dim() == 3 && q->size(0) == total && q->size(2) == d && q->stride(2) == 1 && q->scalar_type() == k.scalar_type() &&
+                q_out->sizes() == q->sizes() && q_out->is_contiguous() && q_out->scalar_type() == q->scalar_type(),
+            "q must be [tokens, heads, head_dim] with contiguous vectors, q_out contiguous, both of the rows' dtype");
+    const at::Tensor* cu = a[3] == Py_None ? nullptr : &int32s(a[3], batch + 1, "cu_seqlens must be a contiguous int32 tensor [batch + 1]");
+    const at::Tensor* offsets = a[6] == Py_None ? nullptr : &int32s(a[6], batch, "offsets must be a contiguous int32 tensor [batch]");
+    check(freq == nullptr || (freq->scalar_type() == at::kDouble && freq->is_contiguous() && freq->dim() == 1), "frequencies must be a contiguous float64 tensor");
+    check(status.scalar_type() == at::kInt && status.is_contiguous() && status.numel() >= PQ_STATUS_WORDS, "status must hold the status words");
+    const c10::Device device = one_device({&k, &v, q, q_out, cu, offsets, freq, &lens, &status, &pool.pool});
+    const c10::cuda::CUDAGuard guard(device);
+    const int64_t rotary = freq == nullptr ? 0 : 2 * freq->size(0);
+    check(rotary <= d && total <= INT32_MAX && batch <= INT32_MAX && k.size(1) <= INT32_MAX, "rotary dimensions within the head, sizes within 32 bits");
+    const int interleaved = PyObject_IsTrue(a[5]);
+    if (interleaved < 0) throw PyError();
+    return call(pq_append_window, (int32_t)d, q == nullptr ? 0 : (int32_t)q->size(1), (int32_t)k.size(1), q == nullptr ? nullptr : ptr(*q), ptr(k), ptr(v),
+                dtype_code(k), q == nullptr ? 0 : q->stride(0), q == nullptr ? 0 : q->stride(1), k.stride(0), k.stride(1),
+                cu == nullptr ? nullptr : ptr<int32_t>(*cu), (int32_t)batch, (int32_t)total, rotary == 0 ? nullptr : ptr<double>(*freq), (int32_t)rotary,
+                (int32_t)interleaved, offsets == nullptr ? nullptr : ptr<int32_t>(*offsets), q == nullptr ? nullptr : ptr(*q_out), ptr(pool.pool),
+                ptr<int32_t>(lens), pool.paging.get(), ptr<int32_t>(status), stream_on(device, a[12]));
+  });
+}
+
+// window_attend(q, pool, lens, max_len, scale, out, lse or None, workspace, status, paging, stream): q [batch, heads, d] or [batch, queries, heads, d]
+PyObject* window_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 11, [&]() -> int32_t {
+    const at::Tensor &q = tensor(a[0]), &out = tensor(a[5]), &ws = tensor(a[7]), &status = tensor(a[8]);
+    const bool multi = q.dim() == 4;
+    check_query(q, out, multi ? 4 : 3);
+    const int64_t batch = q.size(0), n_q = multi ? q.size(1) : 1, hq = q.size(-2), d = q.size(-1);
+    const PoolArg pool(a[1], a[9], batch, d);
+    const at::Tensor& lens = int32s(a[2], batch, "lens must be a contiguous int32 tensor [batch]");
+    const at::Tensor* lse = tensor_or_none(a[6]);
+    check(lse == nullptr || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->sizes() == q.sizes().slice(0, q.dim() - 1)),
+          "lse must be a contiguous float32 tensor of q's shape without the last dimension");
+    check(status.scalar_type() == at::kInt && status.is_contiguous() && status.numel() >= PQ_STATUS_WORDS, "status must hold the status words");
+    const int32_t most = i32(a[3]);
+    check(batch <= INT32_MAX && n_q <= INT32_MAX && hq <= INT32_MAX, "sizes within 32 bits");
+    const int64_t need = pq_window_workspace_bytes((int32_t)d, (int32_t)batch, (int32_t)n_q, (int32_t)hq, (int32_t)pool.pool.size(1), most);
+    check(need < 0 || (ws.is_contiguous() && (int64_t)ws.nbytes() >= need), "the workspace is too small");   // below 0: the call itself says why
+    const c10::Device device = one_device({&q, &out, lse, &ws, &status, &lens, &pool.pool});
+    const c10::cuda::CUDAGuard guard(device);
+    return call(pq_window_attention, (int32_t)d, (int32_t)hq, (int32_t)pool.pool.size(1), ptr(q), dtype_code(q), ptr(pool.pool), dtype_code(pool.pool),
+                ptr<int32_t>(lens), (int32_t)batch, (int32_t)n_q, pool.paging.get(), most, f32(a[4]), ptr(out),
+                lse == nullptr ? nullptr : ptr<float>(*lse), ptr(ws), ptr<int32_t>(status), stream_on(device, a[10]));
+  });
+}
+
 PyMethodDef kMethods[] = {
+    {"append_window", (PyCFunction)(void (*)(void))append_window, METH_FASTCALL, nullptr},
+    {"window_attend", (PyCFunction)(void (*)(void))window_attend, METH_FASTCALL, nullptr},
     {"angle_histograms", (PyCFunction)(void (*)(void))angle_histograms, METH_FASTCALL, nullptr},
     {"tail_attend", (PyCFunction)(void (*)(void))tail_attend, METH_FASTCALL, nullptr},
     {"merge", (PyCFunction)(void (*)(void))merge, METH_FASTCALL, nullptr},

@@ -295,6 +295,28 @@ inline int32_t launch_status() {
   return PQ_ERR_CUDA;
 }
 
+// Launches `kernel` as a programmatic dependent (it waits inside for the kernel before it in the stream).
+template <class... Params, class... Args>
+static int32_t launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+  if (e != cudaSuccess) {
+    note_cuda_error(e);
+    cudaGetLastError();
+    return PQ_ERR_CUDA;
+  }
+  return launch_status();
+}
+
 // One-time, per-device launch configuration of a kernel that needs more than 48 KB of dynamic shared
 // memory (or, `big_clusters`, clusters of more than 8 blocks): the attribute belongs to the (kernel, device)
 // pair, so the memo is indexed by the current device. `state` is a zero-initialised array the caller keeps per kernel; an entry holds the device's

@@ -570,6 +570,7 @@ __global__ void __launch_bounds__(kTailThreads) tail_attention_kernel(const __gr
 
 }  // namespace pq
 #include "pq_tail_mma.cuh"
+#include "pq_window_attention.cuh"
 namespace pq {
 
 // ---- inspection kernels ----------------------------------------------------------------------
@@ -1173,6 +1174,50 @@ int32_t pq_dequant_kv_paged(int32_t head_dim, int32_t n_kv_heads, const float* S
   if (st != PQ_OK) return st;
   return dequant_entry(head_dim, n_kv_heads, S_dev, tables_dev, cache_dev, batch, pg.page_tokens * pg.pages_per_seq, pg,
                        n_tokens, x_hat_dev, stream);
+}
+
+
+int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len) {
+  if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
+  if (batch <= 0 || n_q <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_len <= 0 || n_q_heads % n_kv_heads) return PQ_ERR_INVALID_ARG;
+  const int64_t rows = (int64_t)batch * n_q * n_q_heads;
+  const int64_t units = (int64_t)batch * n_kv_heads * pq::window_row_blocks(n_q, n_q_heads / n_kv_heads);
+  const pq::WindowCut cut = pq::cut_window(units, max_len, pq::kFastMaxGridHost);
+  return cut.parts > 1 ? cut.parts * rows * (head_dim + 1) * 4 : 16;
+}
+
+int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
+                            const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
+                            const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
+                            void* workspace_dev, int32_t* status_dev, void* stream) {
+  pq::NvtxRange nvtx_range("pq_window_attention");
+  if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
+  if (!q_dev || !pool_dev || !window_lens_dev || !out_dev || !workspace_dev || !status_dev) return PQ_ERR_INVALID_ARG;
+  if (batch <= 0 || n_q <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_len <= 0 || n_q_heads % n_kv_heads) return PQ_ERR_INVALID_ARG;
+  if ((io_dtype != PQ_DTYPE_F32 && io_dtype != PQ_DTYPE_BF16) || (kv_dtype != PQ_DTYPE_F32 && kv_dtype != PQ_DTYPE_BF16)) return PQ_ERR_UNSUPPORTED;
+  pq::WindowArgs a;
+  int32_t st = pq::window_paging_from(paging, &a.pg);
+  if (st != PQ_OK) return st;
+  if (((uintptr_t)q_dev | (uintptr_t)pool_dev | (uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
+  if (((uintptr_t)window_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
+  const int g = n_q_heads / n_kv_heads;
+  const int64_t row_blocks = pq::window_row_blocks(n_q, g);
+  if (batch > 65535 || n_kv_heads * row_blocks > 65535) return PQ_ERR_UNSUPPORTED;
+  static pq::DeviceMemo sm_count;
+  const int n_sm = pq::sm_count_of_device(sm_count);
+  if (n_sm == 0) return PQ_ERR_CUDA;
+  const pq::WindowCut cut = pq::cut_window(batch * n_kv_heads * row_blocks, max_len, std::min(n_sm, pq::kFastMaxGridHost));
+  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype;
+  a.row_blocks = (int)row_blocks; a.n_parts = cut.parts; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
+  a.q = q_dev; a.pool = reinterpret_cast<const uint8_t*>(pool_dev); a.lens = window_lens_dev; a.out = out_dev; a.lse = lse_dev;
+  a.part_out = reinterpret_cast<float*>(workspace_dev); a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * head_dim : 0);
+  a.status = status_dev;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int rows = pq::window_block_rows((int64_t)n_q * g);
+  st = kv_dtype == PQ_DTYPE_BF16 ? pq::launch_window_dim<__nv_bfloat16>(a, rows, batch, cut, s) : pq::launch_window_dim<float>(a, rows, batch, cut, s);
+  if (st != PQ_OK || cut.parts == 1) return st;
+  // the window kernel has reported the rows that see nothing
+  return pq::launch_merge(head_dim, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, out_dev, io_dtype, lse_dev, nullptr, s);
 }
 
 }  // extern "C"

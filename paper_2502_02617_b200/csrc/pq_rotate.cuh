@@ -287,28 +287,6 @@ __global__ void __launch_bounds__(kRotThreads) merge_rows_kernel(const float* S,
   store_unrotated<kTile>(x, s, row0, n_rows, lane, warp, a.out, a.io_dtype);
 }
 
-// Launches `kernel` as a programmatic dependent (it waits inside for the kernel before it in the stream).
-template <class... Params, class... Args>
-static int32_t launch_dependent(void (*kernel)(Params...), dim3 grid, int threads, int smem, cudaStream_t stream, Args... args) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
-  if (e != cudaSuccess) {
-    note_cuda_error(e);
-    cudaGetLastError();
-    return PQ_ERR_CUDA;
-  }
-  return launch_status();
-}
-
 // `launch` with the tile for the number of rows as a constant, and the device's SMs.
 template <class Launch>
 static int32_t with_rot_tile(int64_t n_rows, Launch launch) {
