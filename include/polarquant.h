@@ -453,6 +453,41 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
                             void* workspace_dev, int32_t* status_dev, void* stream);
 
 /*
+ * A prefix that the sequences of a batch share (a system prompt, a document with many questions about it), held once in the
+ * packed cache and attended once for all.
+ *
+ * pq_prefix_attention: every one of n_queries queries attends (Eq. 3) to ALL cached tokens of one sequence of a packed cache
+ * (paging == NULL: the contiguous cache of `capacity` tokens, else the paged cache and `capacity` is ignored).  A token is
+ * decoded once for up to 32 or up to 256 (query, head) rows at head_dim 128, whichever is faster, and at other head_dims for
+ * the heads of one query.
+ *   q_dev, out_dev    [n_queries][n_q_heads][head_dim] of io_dtype; n_queries at most 65535
+ *   cache_lens_dev    int32[cache_batch], the cache's; the queries see the cache_lens[sequence] tokens of `sequence`
+ *   max_len           host-side upper bound on that length
+ *   lse_dev           float32 [n_queries][n_q_heads] or NULL; with it an empty prefix yields zeros and -inf and is no error
+ *   workspace_dev     pq_workspace_bytes(head_dim, n_queries, n_q_heads, n_kv_heads, max_len) bytes
+ * Tolerances are those of pq_multi_query_attention.
+ *
+ * pq_shared_attention: the last n_q positions of every sequence attend to the shared prefix and, causally, to their own paged
+ * window behind it (pq_window_attention): one softmax over both.  q_dev, out_dev [batch][n_q][n_q_heads][head_dim].  The
+ * partial results are float32 and merged by their log-sum-exps.  A query that sees no token yields zeros and records
+ * PQ_ERR_EMPTY.  workspace_dev: pq_shared_workspace_bytes(...) bytes; two calls that overlap in time must not share it.
+ */
+int32_t pq_prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
+                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
+                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                            int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* out_dev,
+                            float* lse_dev, void* workspace_dev, int32_t* status_dev, void* stream);
+int64_t pq_shared_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads,
+                                  int32_t max_len, int32_t max_window);
+int32_t pq_shared_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
+                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t batch, int32_t n_q,
+                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                            int32_t capacity, const pq_paging* paging, int32_t max_len, const void* pool_dev,
+                            int32_t kv_dtype, const int32_t* window_lens_dev, const pq_paging* window_paging,
+                            int32_t max_window, float scale, void* out_dev, void* workspace_dev, int32_t* status_dev,
+                            void* stream);
+
+/*
  * General recursion depth and bit tables.  Definition 1 recurses log2 d times and Section 4 counts
  * b_FPN + (d - 1) b bits per vector for b bits per angle; Section 4.1 stops at L = 4 with (4,2,2,2) bits, which the
  * entry points above implement at speed.  The pq_general_* entry points take any head_dim = 2^k <= 256, any

@@ -75,6 +75,12 @@ _SIGNATURES = {
     "pq_window_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32]),
     "pq_window_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_int32,
                                       c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "pq_prefix_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32,
+                                      c_int32, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "pq_shared_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32]),
+    "pq_shared_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_int32, c_void_p, c_void_p,
+                                      c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_int32, c_float,
+                                      c_void_p, c_void_p, c_void_p, c_void_p]),
     "pq_general_sizes": (c_int32, [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "pq_general_fit_codebooks": (c_int32, [c_void_p, c_void_p, c_void_p]),
     "pq_general_cache_bytes": (c_int64, [c_void_p, c_int32, c_int32, c_int32]),
@@ -414,6 +420,27 @@ def pq_window_attention(q, pool, lens, max_len, scale, out, lse, workspace, stat
     _check((_native or native()).window_attend(q, pool, lens, max_len, scale, out, lse, workspace, status, paging, stream), "pq_window_attention")
 
 
+def pq_prefix_attention(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, lse, workspace, status, paging=None, stream=None):
+    """Every query of q [..., Hq, d] attends to all tokens of sequence `seq` of a packed cache, decoded once for all.  `workspace` must hold
+    pq_workspace_bytes(d, queries, Hq, Hkv, max_len); `paging`: None, or (page table, tokens per page, pages) for a paged cache."""
+    _check((_native or native()).prefix_attend(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, workspace, status, paging,
+                                               stream, lse), "pq_prefix_attention")
+
+
+def pq_shared_workspace_bytes(d: int, batch: int, n_q: int, n_q_heads: int, n_kv_heads: int, max_len: int, max_window: int) -> int:
+    n = int(lib().pq_shared_workspace_bytes(d, batch, n_q, n_q_heads, n_kv_heads, max_len, max_window))
+    if n < 0:
+        raise PolarQuantError(n, "pq_shared_workspace_bytes")
+    return n
+
+
+def pq_shared_attention(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, workspace, status, pool, window_lens,
+                        max_window, window_paging, paging=None, stream=None):
+    """One softmax over a prefix that all sequences share (sequence `seq` of a packed cache) and, causally, each sequence's own paged window."""
+    _check((_native or native()).shared_attend(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, workspace, status, paging,
+                                               stream, pool, window_lens, max_window, window_paging), "pq_shared_attention")
+
+
 def pq_paged_cache_bytes(d: int, n_kv_heads: int, page_tokens: int, n_pages: int) -> int:
     n = int(lib().pq_paged_cache_bytes(d, n_kv_heads, page_tokens, n_pages))
     if n < 0:
@@ -524,6 +551,43 @@ class PolarQuantCache:
             with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, self.device)):
                 ws = self._multi_ws[key] = torch.empty(need, dtype=torch.uint8, device=self.device)   # goes back to the stream that used it
         return ws
+
+    _shared_ws = None     # workspaces of attend_prefix and attend_shared by stream
+    _shared_need = None   # bytes by arguments
+
+    def _shared_workspace(self, stream, size, *args):
+        if self._shared_ws is None:
+            self._shared_ws, self._shared_need = {}, {}
+        need = self._shared_need.get(args)
+        if need is None:
+            need = self._shared_need[args] = size(self.d, *args)
+        return _stream_workspace(self._shared_ws, need, stream, self.device)
+
+    def attend_prefix(self, q, seq=0, out=None, scale=None, max_len=None, lse=None, stream=None):
+        """q [B, Hq, d] or [B, n_q, Hq, d] of any batch: every query attends to all tokens of sequence `seq` of this cache, which
+        are decoded once for all (a prompt that many sequences share).  lse: float32 [B, (n_q,) Hq] to write the log-sum-exps to."""
+        if out is None:
+            with _on(stream, self.device):
+                out = torch.empty_like(q)
+        most = self.capacity if max_len is None else max_len
+        ws = self._shared_workspace(stream, pq_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
+        pq_prefix_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
+                            self.d ** -0.5 if scale is None else scale, out, lse, ws, self.status, self._paging_args(), stream)
+        return out
+
+    def attend_shared(self, q, window, seq=0, out=None, scale=None, max_len=None, max_window=None, stream=None):
+        """q [B, Hq, d], or [B, n_q, Hq, d] for the last n_q positions of every sequence: attention over the shared prefix (sequence `seq`
+        of this cache) followed by the sequence's own tokens in `window` (a PagedWindow of B sequences), causal in the window."""
+        if out is None:
+            with _on(stream, self.device):
+                out = torch.empty_like(q)
+        most, most_window = self.capacity if max_len is None else max_len, window.capacity if max_window is None else max_window
+        ws = self._shared_workspace(stream, pq_shared_workspace_bytes, q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2], self.n_kv_heads,
+                                    most, most_window)
+        pq_shared_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
+                            self.d ** -0.5 if scale is None else scale, out, ws, self.status, window.pool, window.lens, most_window,
+                            window._paging_args(), self._paging_args(), stream)
+        return out
 
     def unpack(self, n_tokens):
         return pq_unpack_codes(self.d, self.n_kv_heads, self.cache, self.batch, self.capacity, n_tokens)

@@ -56,6 +56,7 @@ const T* address(PyObject* o) {
 class PagingArg {
  public:
   explicit PagingArg(PyObject* o) {
+    if (o == Py_None) return;
     if (PyTuple_Check(o)) {
       check(PyTuple_GET_SIZE(o) == 3, "paging is (page table, tokens per page, pages)");
       const at::Tensor& table = tensor(PyTuple_GET_ITEM(o, 0));
@@ -365,7 +366,72 @@ PyObject* window_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// What prefix_attend and shared_attend have in common: (S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, workspace,
+// status, paging, stream, ...); paging None (a contiguous cache of `capacity` tokens) or a tuple
+struct PrefixArgs {
+  const at::Tensor &S, &tables, &q, &cache, &lens, &out, &ws, &status;
+  const PagingArg paging;
+  int32_t seq, hkv, capacity, max_len;
+  float scale;
+  int32_t d, hq;
+  explicit PrefixArgs(PyObject* const* a)
+      : S(tensor(a[0])), tables(tensor(a[1])), q(tensor(a[2])), cache(tensor(a[3])), lens(tensor(a[4])), out(tensor(a[10])), ws(tensor(a[11])),
+        status(tensor(a[12])), paging(a[13]), seq(i32(a[5])), hkv(i32(a[6])), capacity(i32(a[7])), max_len(i32(a[8])), scale(f32(a[9])) {
+    check(q.dim() == 3 || q.dim() == 4, "q must be [batch, heads, head_dim] or [batch, queries, heads, head_dim]");
+    check_query(q, out, q.dim());
+    check(q.numel() <= INT32_MAX && q.numel() > 0, "queries within 31 bits of elements");
+    d = (int32_t)q.size(-1);
+    hq = (int32_t)q.size(-2);
+    check(S.scalar_type() == at::kFloat && S.is_contiguous() && S.dim() == 2 && S.size(0) == d && S.size(1) == d, "S must be a float32 tensor [head_dim, head_dim]");
+    check(lens.scalar_type() == at::kInt && lens.is_contiguous() && lens.dim() == 1, "lens must be a contiguous int32 tensor [batch]");
+    check(ws.is_contiguous() && status.scalar_type() == at::kInt && status.is_contiguous() && status.numel() >= PQ_STATUS_WORDS, "workspace and status words");
+    const pq_paging* pg = paging.get();
+    const int64_t bytes = pg != nullptr ? pq_paged_cache_bytes(d, hkv, pg->page_tokens, pg->n_pages) : pq_cache_bytes(d, (int32_t)lens.size(0), hkv, capacity);
+    check(bytes < 0 || (cache.is_contiguous() && (int64_t)cache.nbytes() >= bytes), "the cache is smaller than its sizes say");   // below 0: the call says why
+    if (pg != nullptr) check(tensor(PyTuple_GET_ITEM(a[13], 0)).size(0) == lens.size(0), "the page table must have a row for every length");
+  }
+  int32_t queries() const { return (int32_t)(q.numel() / ((int64_t)d * hq)); }
+};
+
+// prefix_attend(..., lse or None): q of any number of queries, all of which see all tokens of sequence `seq` of the cache
+PyObject* prefix_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 16, [&]() -> int32_t {
+    const PrefixArgs p(a);
+    const at::Tensor* lse = tensor_or_none(a[15]);
+    check(lse == nullptr || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->sizes() == p.q.sizes().slice(0, p.q.dim() - 1)),
+          "lse must be a contiguous float32 tensor of q's shape without the last dimension");
+    const int64_t need = pq_workspace_bytes(p.d, p.queries(), p.hq, p.hkv, p.max_len);
+    check(need < 0 || (int64_t)p.ws.nbytes() >= need, "the workspace is too small");   // below 0: the call itself says why
+    const c10::Device device = one_device({&p.q, &p.S, &p.tables, &p.cache, &p.lens, &p.out, &p.ws, &p.status, lse});
+    const c10::cuda::CUDAGuard guard(device);
+    return call(pq_prefix_attention, p.d, p.hq, p.hkv, ptr<float>(p.S), ptr(p.tables), ptr(p.q), dtype_code(p.q), p.queries(), ptr(p.cache),
+                ptr<int32_t>(p.lens), (int32_t)p.lens.size(0), p.seq, p.capacity, p.paging.get(), p.max_len, p.scale, ptr(p.out),
+                lse == nullptr ? nullptr : ptr<float>(*lse), ptr(p.ws), ptr<int32_t>(p.status), stream_on(device, a[14]));
+  });
+}
+
+// shared_attend(..., pool, window_lens, max_window, window_paging)
+PyObject* shared_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return entry(n, 19, [&]() -> int32_t {
+    const PrefixArgs p(a);
+    const int32_t batch = (int32_t)p.q.size(0), n_q = p.q.dim() == 4 ? (int32_t)p.q.size(1) : 1, max_window = i32(a[17]);
+    const PoolArg pool(a[15], a[18], batch, p.d);
+    const at::Tensor& window_lens = int32s(a[16], batch, "the window's lens must be a contiguous int32 tensor [batch]");
+    check(pool.pool.size(1) == p.hkv, "the window must have the cache's kv heads");
+    const int64_t need = pq_shared_workspace_bytes(p.d, batch, n_q, p.hq, p.hkv, p.max_len, max_window);
+    check(need < 0 || (int64_t)p.ws.nbytes() >= need, "the workspace is too small");
+    const c10::Device device = one_device({&p.q, &p.S, &p.tables, &p.cache, &p.lens, &p.out, &p.ws, &p.status, &pool.pool, &window_lens});
+    const c10::cuda::CUDAGuard guard(device);
+    return call(pq_shared_attention, p.d, p.hq, p.hkv, ptr<float>(p.S), ptr(p.tables), ptr(p.q), dtype_code(p.q), batch, n_q, ptr(p.cache),
+                ptr<int32_t>(p.lens), (int32_t)p.lens.size(0), p.seq, p.capacity, p.paging.get(), p.max_len, ptr(pool.pool), dtype_code(pool.pool),
+                ptr<int32_t>(window_lens), pool.paging.get(), max_window, p.scale, ptr(p.out), ptr(p.ws), ptr<int32_t>(p.status),
+                stream_on(device, a[14]));
+  });
+}
+
 PyMethodDef kMethods[] = {
+    {"prefix_attend", (PyCFunction)(void (*)(void))prefix_attend, METH_FASTCALL, nullptr},
+    {"shared_attend", (PyCFunction)(void (*)(void))shared_attend, METH_FASTCALL, nullptr},
     {"append_window", (PyCFunction)(void (*)(void))append_window, METH_FASTCALL, nullptr},
     {"window_attend", (PyCFunction)(void (*)(void))window_attend, METH_FASTCALL, nullptr},
     {"angle_histograms", (PyCFunction)(void (*)(void))angle_histograms, METH_FASTCALL, nullptr},

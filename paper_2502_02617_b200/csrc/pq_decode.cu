@@ -117,7 +117,8 @@ __host__ inline RowCut cut_rows(int64_t all_rows) {
 }
 
 struct DecodeArgs {
-  int d, n_q_heads, n_kv_heads, batch, capacity, io_dtype;
+  int d, n_q_heads, n_kv_heads, batch, capacity, io_dtype, out_dtype;   // of q and of out
+  int causal;  // 0: every query sees all tokens of its sequence (a prefix that the queries' own sequences share)
   int n_q;  // queries per sequence (1: decode).  `batch` counts (sequence, query) pairs: q and out are
             // [batch][n_q_heads][d] with pair p = sequence * n_q + query; `lens` and the cache are per sequence.
   const __half* qrot;  // of prefill_tc_kernel and rows_attention_kernel: the rotated queries [batch][n_q_heads][value | residual][128]
@@ -142,12 +143,14 @@ struct DecodeArgs {
   int32_t* status;
   Workspace ws;
   Paging pg;  // where the cache's token-blocks live
-  // Sequence of (sequence, query) pair p, and the cached tokens its query sees: query j of the n_q last positions of
-  // a sequence attends to the tokens before and at its own position (Section 4: the i-th query sees i tokens).
+  // Tokens at the end of a sequence that query j of its n_q last positions does not see: it attends to the tokens before and at its
+  // own position (Section 4: the i-th query sees i tokens).
+  __device__ __forceinline__ int hidden(int j) const { return causal ? n_q - 1 - j : 0; }
+  // Sequence of (sequence, query) pair p, and the cached tokens its query sees.
   __device__ __forceinline__ int seq_of(int p) const { return n_q == 1 ? p : p / n_q; }
   __device__ __forceinline__ int visible_len(int p) const {
     if (n_q == 1) return lens[p];
-    const int b = p / n_q, v = lens[b] - (n_q - 1 - (p - b * n_q));
+    const int b = p / n_q, v = lens[b] - hidden(p - b * n_q);
     return v > 0 ? v : 0;
   }
 };
@@ -171,7 +174,7 @@ struct PackedSplit {
   static constexpr int kNb = D / 16, kB1 = 4 * kNb, kB2 = kNb, kB3 = kNb >= 2 ? kNb / 2 : 1, kB4 = kNb >= 4 ? kNb / 4 : 1, kBr = 2 * kNb;
   static constexpr int kRow = kB1 + kB2 + kB3 + kB4 + kBr, kBlockBytes = kTokenBlock * kRow;
   SplitCommon c;
-  int n_q;
+  int n_q, causal;
   int64_t head_bytes;
   const Tables* tables;
   const uint8_t* cache;
@@ -184,7 +187,7 @@ struct PackedSplit {
   __host__ __device__ static constexpr int tile_tokens() { return D <= kU ? 32 : 16; }
   static int tile_bytes(int n) { return n * kRow; }
   __device__ __forceinline__ int len(int pair) const {
-    const int b = pair / n_q, v = lens[b] - (n_q - 1 - (pair - b * n_q));
+    const int b = pair / n_q, v = lens[b] - (causal ? n_q - 1 - (pair - b * n_q) : 0);
     return v > 0 ? v : 0;
   }
   __device__ __forceinline__ void fill_tables(float2* tab, int tid) const {
@@ -290,10 +293,10 @@ struct PackedSplit {
 // 5.91 and 6.08.  At head_dim 32 nothing is gained at 4096 tokens (10.27 and 10.20 us), at 128 the kernel has short contexts only.
 constexpr int kPairTokens = 256;
 template <int D, bool kWithPairs = false>
-static PackedSplit<D, kWithPairs> packed_split(const SplitCommon& c, int n_q, const Tables* tables, const uint8_t* cache, const int32_t* lens,
+static PackedSplit<D, kWithPairs> packed_split(const SplitCommon& c, int n_q, bool causal, const Tables* tables, const uint8_t* cache, const int32_t* lens,
                                                const Paging& pg) {
   PackedSplit<D, kWithPairs> p;
-  p.c = c; p.n_q = n_q; p.tables = tables; p.cache = cache; p.lens = lens; p.pg = pg;
+  p.c = c; p.n_q = n_q; p.causal = causal; p.tables = tables; p.cache = cache; p.lens = lens; p.pg = pg;
   p.head_bytes = make_layout(D, pg.page_tokens).head_bytes;
   return p;
 }
@@ -862,7 +865,7 @@ static int32_t launch_prefill_tc(DecodeArgs a, int batch, int n_q, int n_splits,
   }
   const int32_t main_st = launch_status();
   if (main_st != PQ_OK) return main_st;
-  return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.io_dtype, a.status, stream);
+  return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.out_dtype, a.lse, a.status, stream);
 }
 
 }  // namespace pq
@@ -884,12 +887,18 @@ int64_t pq_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q_heads, i
   return std::max(std::max(cut, one), parts);
 }
 
+// The queries see the whole sequence, and the output may be of another type than they are.
+struct SharedPrefix {
+  int out_dtype;
+};
+
 static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
                                 const void* tables_dev, const void* q_dev, int32_t io_dtype, const void* cache_dev,
                                 const int32_t* cache_lens_dev, int32_t batch, int32_t n_q, int32_t capacity, const pq::Paging& pg,
                                 int32_t max_len, float scale, void* out_dev, void* workspace_dev, int32_t* status_dev,
-                                void* stream, float* lse_dev = nullptr) {
+                                void* stream, float* lse_dev = nullptr, const SharedPrefix* shared = nullptr) {
   pq::NvtxRange nvtx_range("pq attention");
+  const bool causal = shared == nullptr;
   if (!(head_dim == 16 || head_dim == 32 || head_dim == 64 || head_dim == 128)) return PQ_ERR_UNSUPPORTED;
   if (!S_dev || !tables_dev || !q_dev || !cache_dev || !cache_lens_dev || !out_dev || !workspace_dev || !status_dev)
     return PQ_ERR_INVALID_ARG;
@@ -904,8 +913,8 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   if (pairs > 65535 || n_kv_heads > 65535) return PQ_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   pq::DecodeArgs a;
-  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.batch = (int)pairs; a.n_q = n_q; a.capacity = capacity;
-  a.io_dtype = io_dtype; a.scale = scale; a.S = S_dev; a.tables = reinterpret_cast<const pq::Tables*>(tables_dev);
+  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.batch = (int)pairs; a.n_q = n_q; a.causal = causal; a.capacity = capacity;
+  a.io_dtype = io_dtype; a.out_dtype = shared ? shared->out_dtype : io_dtype; a.scale = scale; a.S = S_dev; a.tables = reinterpret_cast<const pq::Tables*>(tables_dev);
   a.q = q_dev; a.cache = reinterpret_cast<const uint8_t*>(cache_dev); a.lens = cache_lens_dev; a.out = out_dev;
   a.status = status_dev;
   a.lse = lse_dev;
@@ -913,16 +922,16 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   a.ws = pq::carve_workspace(workspace_dev, head_dim, pairs * n_kv_heads, n_q_heads / n_kv_heads);
   a.rows_per_block = a.n_row_blocks = 0; a.n_splits = 1; a.part_out = a.part_lse = nullptr; a.qrot = nullptr; a.unit_parts = nullptr; a.epoch = a.debug = 0u;
   const int g = n_q_heads / n_kv_heads;
-  if (lse_dev != nullptr && n_q != 1) return PQ_ERR_UNSUPPORTED;
+  if (lse_dev != nullptr && n_q != 1 && causal) return PQ_ERR_UNSUPPORTED;
   pq::SplitCommon c;
-  c.d = head_dim; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = io_dtype; c.scale = scale;
+  c.d = head_dim; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = io_dtype; c.out_dtype = a.out_dtype; c.scale = scale;
   c.S = S_dev; c.q = q_dev; c.out = out_dev; c.lse = lse_dev; c.status = status_dev;
   if (head_dim == 128) {
     const bool paged = pg.table != nullptr;
     static pq::DeviceMemo sm_count;
     const int n_sm = pq::sm_count_of_device(sm_count);
     if (n_sm == 0) return PQ_ERR_CUDA;
-    if (n_q * g >= pq::kPfRows && pq::take_debug_wait_failure(3)) {
+    if (causal && n_q * g >= pq::kPfRows && pq::take_debug_wait_failure(3)) {
       // the register-fragment kernel: decode each block of the cache once for 64 (query, head) rows; only reached here (it is
       // slower than the tcgen05 kernel at every size)
       static pq::DeviceMemo configured_pf;
@@ -932,11 +941,11 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
       pq::prefill_attention_kernel<<<grid, pq::kPfThreads, pq::kPfTotal, st>>>(a, n_q);
       return pq::launch_status();
     }
-    pq::PackedSplit<128> split = pq::packed_split<128>(c, n_q, a.tables, a.cache, cache_lens_dev, pg);
+    pq::PackedSplit<128> split = pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg);
     pq::size_split(split);
     pq::SplitLoad load = {};
     if (pq::plan_split(split, pairs, max_len, &load) == 0) return PQ_ERR_CUDA;
-    const bool tensor = lse_dev == nullptr && pq::window_as_mapped() && !pq::take_debug_wait_failure(10);
+    const bool tensor = (lse_dev == nullptr || !causal) && pq::window_as_mapped() && !pq::take_debug_wait_failure(10);
     pq::AttentionPlan plan = pq::plan_attention(batch, n_q, n_kv_heads, g, max_len, n_sm, load, tensor && n_q * g >= 32);
     if (const int named = pq::take_debug_hook(6, 9)) {   // test hook: the kernel is named
       plan.kernel = named == 6 ? pq::kClusterKernel : named == 7 ? pq::kPersistentKernel : named == 8 ? pq::kRowsKernel : pq::kTensorKernel;
@@ -960,17 +969,17 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     }
   }
   switch (head_dim) {
-    case 16: return pq::dispatch_split_attention(pq::packed_split<16>(c, n_q, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
-    case 32: return pq::dispatch_split_attention(pq::packed_split<32>(c, n_q, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
+    case 16: return pq::dispatch_split_attention(pq::packed_split<16>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
+    case 32: return pq::dispatch_split_attention(pq::packed_split<32>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
     case 64: {
-      auto split = pq::packed_split<64>(c, n_q, a.tables, a.cache, cache_lens_dev, pg);
+      auto split = pq::packed_split<64>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg);
       pq::size_split(split);
       pq::SplitLoad load = {};
       if (pq::plan_split(split, pairs, max_len, &load) == 0) return PQ_ERR_CUDA;
       if (load.waves * load.tokens < pq::kPairTokens) return pq::dispatch_split_attention(split, pairs, max_len, st);
-      return pq::dispatch_split_attention(pq::packed_split<64, true>(c, n_q, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
+      return pq::dispatch_split_attention(pq::packed_split<64, true>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
     }
-    default: return pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
+    default: return pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
   }
 }
 
@@ -1186,10 +1195,10 @@ int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, 
   return cut.parts > 1 ? cut.parts * rows * (head_dim + 1) * 4 : 16;
 }
 
-int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
+static int32_t window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
                             const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
                             const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
-                            void* workspace_dev, int32_t* status_dev, void* stream) {
+                            void* workspace_dev, int32_t* status_dev, void* stream, int out_dtype, bool only_check = false) {
   pq::NvtxRange nvtx_range("pq_window_attention");
   if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
   if (!q_dev || !pool_dev || !window_lens_dev || !out_dev || !workspace_dev || !status_dev) return PQ_ERR_INVALID_ARG;
@@ -1203,11 +1212,12 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
   const int g = n_q_heads / n_kv_heads;
   const int64_t row_blocks = pq::window_row_blocks(n_q, g);
   if (batch > 65535 || n_kv_heads * row_blocks > 65535) return PQ_ERR_UNSUPPORTED;
+  if (only_check) return PQ_OK;
   static pq::DeviceMemo sm_count;
   const int n_sm = pq::sm_count_of_device(sm_count);
   if (n_sm == 0) return PQ_ERR_CUDA;
   const pq::WindowCut cut = pq::cut_window(batch * n_kv_heads * row_blocks, max_len, std::min(n_sm, pq::kFastMaxGridHost));
-  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype;
+  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype;
   a.row_blocks = (int)row_blocks; a.n_parts = cut.parts; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
   a.q = q_dev; a.pool = reinterpret_cast<const uint8_t*>(pool_dev); a.lens = window_lens_dev; a.out = out_dev; a.lse = lse_dev;
   a.part_out = reinterpret_cast<float*>(workspace_dev); a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * head_dim : 0);
@@ -1217,7 +1227,103 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
   st = kv_dtype == PQ_DTYPE_BF16 ? pq::launch_window_dim<__nv_bfloat16>(a, rows, batch, cut, s) : pq::launch_window_dim<float>(a, rows, batch, cut, s);
   if (st != PQ_OK || cut.parts == 1) return st;
   // the window kernel has reported the rows that see nothing
-  return pq::launch_merge(head_dim, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, out_dev, io_dtype, lse_dev, nullptr, s);
+  return pq::launch_merge(head_dim, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, out_dev, out_dtype, lse_dev, nullptr, s);
+}
+
+
+int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
+                            const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
+                            const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
+                            void* workspace_dev, int32_t* status_dev, void* stream) {
+  return window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, paging, max_len, scale,
+                          out_dev, lse_dev, workspace_dev, status_dev, stream, io_dtype);
+}
+
+static int32_t prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
+                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
+                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                            int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* out_dev,
+                            float* lse_dev, void* workspace_dev, int32_t* status_dev, void* stream, int out_dtype) {
+  if (cache_batch <= 0 || sequence < 0 || sequence >= cache_batch || !cache_dev || !cache_lens_dev) return PQ_ERR_INVALID_ARG;
+  if (((uintptr_t)cache_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
+  pq::Paging pg;
+  const uint8_t* cache = reinterpret_cast<const uint8_t*>(cache_dev);
+  if (paging == nullptr) {   // the sequence's own part of the cache, as a cache of one sequence
+    const int64_t before = pq_cache_bytes(head_dim, 1, n_kv_heads, capacity);
+    if (before < 0) return (int32_t)before;
+    cache += before * sequence;
+    pg = pq::contiguous_paging(capacity, 1);
+  } else {
+    const int32_t st = pq::paging_from(paging, head_dim, &pg);
+    if (st != PQ_OK) return st;
+    pg.table += (int64_t)sequence * pg.pages_per_seq;
+    capacity = pg.page_tokens * pg.pages_per_seq;
+  }
+  const SharedPrefix shared = {out_dtype};
+  return launch_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, cache, cache_lens_dev + sequence, 1, n_queries,
+                          capacity, pg, max_len, scale, out_dev, workspace_dev, status_dev, stream, lse_dev, &shared);
+}
+
+int32_t pq_prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
+                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
+                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                            int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* out_dev,
+                            float* lse_dev, void* workspace_dev, int32_t* status_dev, void* stream) {
+  return prefix_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, n_queries, cache_dev, cache_lens_dev, cache_batch,
+                          sequence, capacity, paging, max_len, scale, out_dev, lse_dev, workspace_dev, status_dev, stream, io_dtype);
+}
+
+// The workspace of pq_shared_attention: two parts of float32 outputs with their log-sum-exps, then what the two attentions need.
+struct SharedWorkspace {
+  int64_t lse, prefix, window, bytes;
+};
+static SharedWorkspace shared_workspace(int32_t head_dim, int64_t rows, int64_t prefix_bytes, int64_t window_bytes) {
+  auto align = [](int64_t x) { return (x + 255) & ~(int64_t)255; };
+  SharedWorkspace w;
+  w.lse = align(2 * rows * head_dim * 4);
+  w.prefix = w.lse + align(2 * rows * 4);
+  w.window = w.prefix + align(prefix_bytes);
+  w.bytes = w.window + align(window_bytes);
+  return w;
+}
+int64_t pq_shared_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len,
+                                  int32_t max_window) {
+  if (batch <= 0 || n_q <= 0 || (int64_t)batch * n_q > 65535) return batch <= 0 || n_q <= 0 ? PQ_ERR_INVALID_ARG : PQ_ERR_UNSUPPORTED;
+  const int64_t prefix = pq_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len);
+  if (prefix < 0) return prefix;
+  const int64_t window = pq_window_workspace_bytes(head_dim, batch, n_q, n_q_heads, n_kv_heads, max_window);
+  if (window < 0) return window;
+  return shared_workspace(head_dim, (int64_t)batch * n_q * n_q_heads, prefix, window).bytes;
+}
+
+int32_t pq_shared_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
+                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t batch, int32_t n_q,
+                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                            int32_t capacity, const pq_paging* paging, int32_t max_len, const void* pool_dev,
+                            int32_t kv_dtype, const int32_t* window_lens_dev, const pq_paging* window_paging,
+                            int32_t max_window, float scale, void* out_dev, void* workspace_dev, int32_t* status_dev,
+                            void* stream) {
+  pq::NvtxRange nvtx_range("pq_shared_attention");
+  const int64_t bytes = pq_shared_workspace_bytes(head_dim, batch, n_q, n_q_heads, n_kv_heads, max_len, max_window);
+  if (bytes < 0) return (int32_t)bytes;
+  if (!out_dev || !workspace_dev) return PQ_ERR_INVALID_ARG;
+  if (((uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
+  const int64_t rows = (int64_t)batch * n_q * n_q_heads;
+  const SharedWorkspace at = shared_workspace(head_dim, rows, pq_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len), 0);
+  uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
+  float* parts = reinterpret_cast<float*>(ws);
+  float* lse = reinterpret_cast<float*>(ws + at.lse);
+  // nothing is launched where the window's arguments are refused
+  int32_t st = window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, window_paging,
+                                max_window, scale, parts + rows * head_dim, lse + rows, ws + at.window, status_dev, stream, PQ_DTYPE_F32, true);
+  if (st != PQ_OK) return st;
+  st = prefix_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, batch * n_q, cache_dev, cache_lens_dev,
+                                   cache_batch, sequence, capacity, paging, max_len, scale, parts, lse, ws + at.prefix, status_dev, stream, PQ_DTYPE_F32);
+  if (st != PQ_OK) return st;
+  st = window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, window_paging,
+                           max_window, scale, parts + rows * head_dim, lse + rows, ws + at.window, status_dev, stream, PQ_DTYPE_F32);
+  if (st != PQ_OK) return st;
+  return pq::launch_merge(head_dim, rows, 2, parts, PQ_DTYPE_F32, lse, out_dev, io_dtype, nullptr, status_dev, reinterpret_cast<cudaStream_t>(stream));
 }
 
 }  // extern "C"

@@ -615,7 +615,7 @@ __device__ __forceinline__ void combine_and_store(const DecodeArgs& a, int b, in
     const float t = sum_eight_rows(v, lane);
     if ((lane & 3) == 0) {
       const int64_t oidx = (h0 + h) * 128 + i0 + (lane >> 2);
-      if (a.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[oidx] = __float2bfloat16(t);
+      if (a.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[oidx] = __float2bfloat16(t);
       else reinterpret_cast<float*>(a.out)[oidx] = t;
     }
   }
@@ -703,7 +703,7 @@ __global__ void __launch_bounds__(kFastThreads, 1) decode_attention_fast_kernel(
 #pragma unroll 1
     for (int e = 0; e < g_heads * 128; ++e) {
       const int64_t idx = ((int64_t)b * a.n_q_heads + hk * g_heads) * 128 + e;
-      if (a.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(0.f);
+      if (a.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(0.f);
       else reinterpret_cast<float*>(a.out)[idx] = 0.f;
     }
     if (a.lse != nullptr)

@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kPfThreads) prefill_attention_kernel(DecodeArg
     for (int j0 = 0; j0 < 128; j0 += 4) pf_rank4(acc, osm, kPfOStride, j0, __ldg(srow + (j0 >> 2)));
     for (int r = 0; r < n_rows; ++r) {
       const int64_t o = row_index(r) + tid;
-      if (a.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[o] = __float2bfloat16(acc[r]);
+      if (a.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[o] = __float2bfloat16(acc[r]);
       else reinterpret_cast<float*>(a.out)[o] = acc[r];
     }
   }

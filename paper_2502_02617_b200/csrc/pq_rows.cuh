@@ -122,7 +122,7 @@ __device__ __forceinline__ void combine_rows(const DecodeArgs& a, const int2* in
   for (int r = 0; r < 4; ++r)
     if (r0 + r < n_rows) {
       const int64_t idx = (int64_t)info[r0 + r].x * 128 + i_out;
-      if (a.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(acc[r]);
+      if (a.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(acc[r]);
       else reinterpret_cast<float*>(a.out)[idx] = acc[r];
     }
 }
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_attention_kernel(DecodeAr
   // rows of a unit's block, tokens its last row sees (query j sees the tokens t < len - (n_q - 1 - j))
   auto unit_rows = [&](int rb) -> int { return min(R, all_rows - rb * R); };
   auto unit_len = [&](int seq, int rb) -> int {
-    const int v = a.lens[seq] - (a.n_q - 1 - (rb * R + unit_rows(rb) - 1) / g_heads);
+    const int v = a.lens[seq] - a.hidden((rb * R + unit_rows(rb) - 1) / g_heads);
     return v > 0 ? v : 0;
   };
   auto stages_of = [&](int u) -> int {
@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_attention_kernel(DecodeAr
 #pragma unroll 1
       for (int e = 0; e < g_heads * 128; ++e) {   // u: sequence and kv head
         const int64_t idx = (int64_t)u * g_heads * 128 + e;
-        if (a.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(0.f);
+        if (a.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(a.out)[idx] = __float2bfloat16(0.f);
         else reinterpret_cast<float*>(a.out)[idx] = 0.f;
         if (a.lse != nullptr && (e & 127) == 0) a.lse[idx >> 7] = -CUDART_INF_F;
       }
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_attention_kernel(DecodeAr
       if (warp == 1) {
         const int row = row0 + min(lane, n_rows - 1), j = row / g_heads;
         info[lane] = make_int2((seq * a.n_q + j) * a.n_q_heads + hk * g_heads + (row - j * g_heads),
-                               lane < n_rows ? a.lens[seq] - (a.n_q - 1 - j) : 0);
+                               lane < n_rows ? a.lens[seq] - a.hidden(j) : 0);
       }
       // q' = (q S) * scale * log2(e) of the rows as fp16 value + residual in fragment order: the fragment of
       // (row group, k-step ks, lane) holds, for column n = lane / 4 (row n / 2 of the group; value or residual), coordinates

@@ -37,7 +37,7 @@ constexpr int kUnitStride = 20;            // floats between the 16-coordinate g
 
 // What the kernel needs beside the layout.
 struct SplitCommon {
-  int d, n_q_heads, n_kv_heads, io_dtype;
+  int d, n_q_heads, n_kv_heads, io_dtype, out_dtype;
   int tile, stage_bytes;   // tokens of a tile, bytes of its staged keys (or values): set by dispatch_split_attention
   float scale;
   const float* S;
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(32 * split_warps(kH), 1) split_attention_kerne
     for (int h = 1; h < kH; ++h) mine_h = lane == h ? sum[h] : mine_h;
     if (lane < grp) {
       const int64_t idx = q0 + lane * d + j0 + jj;
-      if (c.io_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(c.out)[idx] = __float2bfloat16(mine_h);
+      if (c.out_dtype == PQ_DTYPE_BF16) reinterpret_cast<__nv_bfloat16*>(c.out)[idx] = __float2bfloat16(mine_h);
       else reinterpret_cast<float*>(c.out)[idx] = mine_h;
     }
   }

@@ -18,7 +18,7 @@ namespace pq {
 constexpr int kWinThreads = 128, kWinWarps = kWinThreads / 32, kWinMaxCluster = 8, kWinMaxParts = 16;
 
 struct WindowArgs {
-  int d, n_q_heads, n_kv_heads, n_q, io_dtype, row_blocks, n_parts;
+  int d, n_q_heads, n_kv_heads, n_q, io_dtype, out_dtype, row_blocks, n_parts;
   int64_t n_rows;       // batch * n_q * n_q_heads: rows of q, out and of a part
   float scale;
   const void* q;
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
       *reinterpret_cast<float4*>(a.part_out + part * a.n_rows * D + at) = acc;
       if (c == 0) a.part_lse[part * a.n_rows + row] = lse;
     } else {
-      if (a.io_dtype == PQ_DTYPE_BF16) {
+      if (a.out_dtype == PQ_DTYPE_BF16) {
         const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
         *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) =
             make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));

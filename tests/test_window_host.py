@@ -100,3 +100,49 @@ def test_frequencies(rotary, theta):
 def test_bad_frequencies_are_refused(rotary, theta):
     with pytest.raises(pq.PolarQuantError):
         pq.pq_rotary_frequencies(rotary, theta)
+
+
+def prefix(**kw):
+    a = dict(d=128, hq=8, hkv=2, S=GOOD, tables=GOOD, q=GOOD, io=pq.DTYPE_BF16, n=4, cache=GOOD, lens=GOOD, cache_batch=2, seq=1, capacity=256, pg=None,
+             most=200, out=GOOD, lse=None, ws=GOOD, status=GOOD)
+    a.update(kw)
+    return L.pq_prefix_attention(a["d"], a["hq"], a["hkv"], a["S"], a["tables"], a["q"], a["io"], a["n"], a["cache"], a["lens"], a["cache_batch"], a["seq"],
+                                 a["capacity"], ctypes.addressof(a["pg"]) if a["pg"] else None, a["most"], 0.1, a["out"], a["lse"], a["ws"], a["status"], None)
+
+
+PREFIX_REFUSALS = [
+    (dict(d=48), "UNSUPPORTED"), (dict(d=256), "UNSUPPORTED"), (dict(io=5), "UNSUPPORTED"), (dict(hq=36, hkv=2), "UNSUPPORTED"),
+    (dict(q=None), "INVALID_ARG"), (dict(S=None), "INVALID_ARG"), (dict(tables=None), "INVALID_ARG"), (dict(cache=None), "INVALID_ARG"),
+    (dict(lens=None), "INVALID_ARG"), (dict(out=None), "INVALID_ARG"), (dict(ws=None), "INVALID_ARG"), (dict(status=None), "INVALID_ARG"),
+    (dict(seq=-1), "INVALID_ARG"), (dict(seq=2), "INVALID_ARG"), (dict(cache_batch=0), "INVALID_ARG"), (dict(n=0), "INVALID_ARG"), (dict(hq=7), "INVALID_ARG"),
+    (dict(capacity=0), "INVALID_ARG"), (dict(most=0), "INVALID_ARG"), (dict(lens=GOOD + 2), "ALIGNMENT"), (dict(q=GOOD + 8), "ALIGNMENT"),
+    (dict(cache=GOOD + 8), "ALIGNMENT"), (dict(n=65536), "UNSUPPORTED"), (dict(pg=paging(page_tokens=64)), "INVALID_ARG"),
+    (dict(pg=paging(table=GOOD + 1, page_tokens=128)), "ALIGNMENT")]
+
+
+@pytest.mark.parametrize("change,status", PREFIX_REFUSALS)
+def test_prefix_attention_refuses(change, status):
+    assert prefix(**change) == getattr(pq, "ERR_" + status)
+
+
+def shared(window_paging=None, **kw):
+    a = dict(d=128, hq=8, hkv=2, S=GOOD, tables=GOOD, q=GOOD, io=pq.DTYPE_BF16, batch=4, n_q=1, cache=GOOD, lens=GOOD, cache_batch=2, seq=1, capacity=256, pg=None,
+             most=200, pool=GOOD, kv=pq.DTYPE_BF16, wlens=GOOD, most_window=64, out=GOOD, ws=GOOD, status=GOOD)
+    a.update(kw)
+    wpg = paging() if window_paging is None else window_paging
+    return L.pq_shared_attention(a["d"], a["hq"], a["hkv"], a["S"], a["tables"], a["q"], a["io"], a["batch"], a["n_q"], a["cache"], a["lens"], a["cache_batch"],
+                                 a["seq"], a["capacity"], ctypes.addressof(a["pg"]) if a["pg"] else None, a["most"], a["pool"], a["kv"], a["wlens"],
+                                 ctypes.addressof(wpg), a["most_window"], 0.1, a["out"], a["ws"], a["status"], None)
+
+
+@pytest.mark.parametrize("change,status", [(c, s) for c, s in PREFIX_REFUSALS if "n" not in c and "lse" not in c] + [
+    (dict(pool=None), "INVALID_ARG"), (dict(wlens=None), "INVALID_ARG"), (dict(kv=4), "UNSUPPORTED"), (dict(most_window=0), "INVALID_ARG"),
+    (dict(pool=GOOD + 8), "ALIGNMENT"), (dict(wlens=GOOD + 1), "ALIGNMENT"), (dict(batch=0), "INVALID_ARG"), (dict(n_q=0), "INVALID_ARG"),
+    (dict(batch=300, n_q=300), "UNSUPPORTED")])
+def test_shared_attention_refuses(change, status):
+    assert shared(**change) == getattr(pq, "ERR_" + status)
+
+
+@pytest.mark.parametrize("pg,status", BAD_PAGING)
+def test_shared_attention_refuses_a_bad_window(pg, status):
+    assert shared(window_paging=pg) == status
