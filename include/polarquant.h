@@ -417,8 +417,8 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  *                      three may be parts of one projection's rows).  q_dev = NULL: no queries (n_q_heads = 0, q_out = NULL).
  *                      Unlike other device pointers these three, and q_out, need only their element's alignment
  *   q_out_dev          [total_tokens][n_q_heads][head_dim] contiguous; may be q_dev where q is laid out so
- *   cu_seqlens_dev     int32[batch+1] as for pq_encode_kv, but rows behind cu[batch] are allowed and left alone (a padded
- *                      batch: neither read nor written); NULL: row b is sequence b's (total_tokens = batch)
+ *   cu_seqlens_dev     int32[batch+1] as for pq_encode_kv, but rows behind cu[batch] are allowed (a padded batch) and give
+ *                      nothing: neither the window nor q_out is written for them; NULL: row b is sequence b's (total_tokens = batch)
  *   frequencies_dev    float64[rotary_dim / 2], NULL with rotary_dim = 0 (no rotation).  Like S_dev it is read during set-up
  *   interleaved        0: pairs (i, i + rotary_dim / 2); 1: pairs (2i, 2i + 1)
  *   offsets_dev        int32[batch], position of each window's first token (the lengths of a packed cache, say); NULL: 0

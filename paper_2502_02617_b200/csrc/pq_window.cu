@@ -1,5 +1,6 @@
 // The paged window of recent tokens: new rows on their way in, with the rotary position applied to queries and keys.  (The
 // attention that reads it is pq_window_attention.cuh.)
+#include <algorithm>
 #include <cmath>
 
 #include "pq_common.cuh"
@@ -39,20 +40,15 @@ __device__ __forceinline__ int64_t append_target(const AppendArgs& a, int seq, i
   }
   return window_row(a.pg, a.n_kv_heads, a.d, page, 0, 0, place % a.pg.page_tokens);
 }
-__device__ __forceinline__ AppendPlace append_place(const AppendArgs& a, int token) {
-  AppendPlace p = {token, 0, -1};
+// `seq`: a sequence at or before the row's.
+__device__ __forceinline__ AppendPlace append_place(const AppendArgs& a, int token, int seq) {
+  AppendPlace p = {seq, 0, -1};
   int first = token, count = 1;
   if (a.cu_seqlens != nullptr) {
-    int lo = 0, hi = a.batch;   // the first sequence that ends behind the row
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (a.cu_seqlens[mid + 1] > token) hi = mid;
-      else lo = mid + 1;
-    }
-    p.seq = lo;
-    if (lo == a.batch) return p;
-    first = a.cu_seqlens[lo];
-    count = a.cu_seqlens[lo + 1] - first;
+    while (p.seq < a.batch && a.cu_seqlens[p.seq + 1] <= token) ++p.seq;   // the first sequence that ends behind the row
+    if (p.seq >= a.batch) return p;
+    first = a.cu_seqlens[p.seq];
+    count = a.cu_seqlens[p.seq + 1] - first;
   }
   const int base = a.lens[p.seq];
   p.place = base + (token - first);
@@ -78,16 +74,79 @@ __device__ __forceinline__ void store_f32(void* p, int64_t i, float v) {
   reinterpret_cast<T*>(p)[i] = (T)v;
 }
 
+__device__ __forceinline__ uint4 ld_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 bf16_pair(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
+  const __nv_bfloat162 w = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&w);
+}
+// Elements e of x and of y are a pair, with the cosine and sine c[e].
+template <class T>
+__device__ __forceinline__ void turn_halves(uint4& x, uint4& y, const float2* c) {
+  uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 2) {
+      const float2 p = bf16_pair(a[i]), q = bf16_pair(b[i]);
+      const float4 k = *reinterpret_cast<const float4*>(c + 2 * i);
+      a[i] = pair_bf16(p.x * k.x - q.x * k.y, p.y * k.z - q.y * k.w);
+      b[i] = pair_bf16(q.x * k.x + p.x * k.y, q.y * k.z + p.y * k.w);
+    } else {
+      const float p = __uint_as_float(a[i]), q = __uint_as_float(b[i]);
+      const float2 k = c[i];
+      a[i] = __float_as_uint(p * k.x - q * k.y);
+      b[i] = __float_as_uint(q * k.x + p * k.y);
+    }
+  }
+  x = make_uint4(a[0], a[1], a[2], a[3]);
+  y = make_uint4(b[0], b[1], b[2], b[3]);
+}
+// Neighbouring elements are a pair.
+template <class T>
+__device__ __forceinline__ uint4 turn_neighbours(const uint4& v, const float2* c) {
+  uint32_t a[4] = {v.x, v.y, v.z, v.w};
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 p = bf16_pair(a[i]), k = c[i];
+      a[i] = pair_bf16(p.x * k.x - p.y * k.y, p.y * k.x + p.x * k.y);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      const float p = __uint_as_float(a[i]), q = __uint_as_float(a[i + 1]);
+      const float2 k = c[i / 2];
+      a[i] = __float_as_uint(p * k.x - q * k.y);
+      a[i + 1] = __float_as_uint(q * k.x + p * k.y);
+    }
+  }
+  return make_uint4(a[0], a[1], a[2], a[3]);
+}
+
+// The sequence that row `token` belongs to, or one before it.
+__device__ __forceinline__ int sequence_of(const AppendArgs& a, int token) {
+  if (a.cu_seqlens == nullptr) return token;
+  int lo = 0, hi = a.batch;
+  while (lo < hi) {
+    const int mid = (lo + hi) >> 1;
+    if (a.cu_seqlens[mid + 1] > token) hi = mid;
+    else lo = mid + 1;
+  }
+  return lo;
+}
 // A thread takes a pair of elements of one head of one row, whatever the strides and alignments.
 template <class T>
 __global__ void __launch_bounds__(256) append_window_kernel(const __grid_constant__ AppendArgs a) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int pairs = a.d / 2, heads = a.n_q_heads + 2 * a.n_kv_heads;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / pairs;
   if (row >= (int64_t)a.total_tokens * heads) return;
   const int u = (int)(i % pairs), token = (int)(row / heads), head = (int)(row % heads);
-  const AppendPlace p = append_place(a, token);
+  const AppendPlace p = append_place(a, token, sequence_of(a, token));
   if (p.seq >= a.batch) return;
   const bool is_q = head < a.n_q_heads, is_v = head >= a.n_q_heads + a.n_kv_heads;
   const int h = is_q ? head : is_v ? head - a.n_q_heads - a.n_kv_heads : head - a.n_q_heads;
@@ -110,12 +169,8 @@ __global__ void __launch_bounds__(256) append_window_kernel(const __grid_constan
   }
 }
 
-// The windows grow once their rows are in: a thread per sequence.
-__global__ void __launch_bounds__(128) advance_windows_kernel(const __grid_constant__ AppendArgs a) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int b = blockIdx.x * 128 + threadIdx.x;
-  if (b >= a.batch) return;
+// A sequence's window grows by its rows, all of them or, where one of them has no place, none.
+__device__ __forceinline__ void advance_window(const AppendArgs& a, int b) {
   const int base = a.lens[b], count = a.cu_seqlens != nullptr ? a.cu_seqlens[b + 1] - a.cu_seqlens[b] : 1;
   if (count <= 0 || !append_fits(a, base, count)) return;
   if (a.cu_seqlens != nullptr && a.cu_seqlens[b + 1] > a.total_tokens) {   // rows that do not exist
@@ -126,16 +181,129 @@ __global__ void __launch_bounds__(128) advance_windows_kernel(const __grid_const
     if ((unsigned)a.pg.table[(int64_t)b * a.pg.pages_per_seq + p] >= (unsigned)a.pg.n_pages) return;
   a.lens[b] = base + count;
 }
+// A thread per sequence, behind a kernel that has every block say (launch_dependents) when it has read the lengths: the windows
+// grow while the rows are still on their way.  The wait at the end makes this kernel's end that of the rows' too.
+__global__ void __launch_bounds__(128) advance_windows_kernel(const __grid_constant__ AppendArgs a) {
+  const int b = blockIdx.x * 128 + threadIdx.x;
+  if (b < a.batch) advance_window(a, b);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+
+// The rows as 16-byte pieces, where they lie on 16 bytes and the rotated part of a head is a multiple of 32.  An item is two pieces of
+// one head of one row: the two sides of kV rotated pairs, or copied elements.  A block takes kApItems items per thread of a few
+// rows -- all loads go out before anything else --, looks up where its rows go, forms the cosines and sines of each row once for
+// all heads, and stores.  Bound by HBM: 32768 rows of 32/8 heads of 128 in bf16 ...
+constexpr int kApThreads = 256, kApItems = 3, kApTokens = 8, kApMaxHalf = 64;
+template <class T>
+__global__ void __launch_bounds__(kApThreads) append_window_pieces_kernel(const __grid_constant__ AppendArgs a, int tokens, int slices,
+                                                                          bool alone) {
+  constexpr int kV = 16 / sizeof(T);
+  __shared__ float2 cs[kApTokens][kApMaxHalf];
+  __shared__ AppendPlace places[kApTokens];
+  const int tid = threadIdx.x, token0 = blockIdx.x / slices * tokens, slice = blockIdx.x % slices;
+  const int n_tokens = min(tokens, a.total_tokens - token0);
+  const int per_head = a.d / (2 * kV), turns = a.half / kV, rest = (a.d - 2 * a.half) / 2;
+  const int kv_items = a.n_kv_heads * per_head, q_items = a.n_q_heads * per_head, per_token = q_items + 2 * kv_items;
+  const int first = slice * kApThreads * kApItems, n_items = min(n_tokens * per_token, first + kApThreads * kApItems);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  uint4 x[kApItems], y[kApItems];
+  int token[kApItems], to[kApItems], gap[kApItems], turn[kApItems];   // to: element of the row's output (queries) or offset from AppendPlace::at
+  bool is_q[kApItems];
+#pragma unroll
+  for (int k = 0; k < kApItems; ++k) {
+    const int i = first + tid + k * kApThreads;
+    token[k] = -1;
+    if (i >= n_items) continue;
+    const int t = i / per_token, r = i - t * per_token;
+    is_q[k] = r < q_items;
+    const bool is_v = r >= q_items + kv_items;
+    const int rr = is_q[k] ? r : is_v ? r - q_items - kv_items : r - q_items, h = rr / per_head, u = rr - h * per_head;
+    const bool rotated = !is_v && u < turns;
+    const int u2 = is_v ? u : u - turns, behind = is_v ? 0 : 2 * a.half, half_rest = is_v ? a.d / 2 : rest;   // copied elements: two halves
+    const int at = !rotated ? behind + u2 * kV : a.interleaved ? 2 * u * kV : u * kV;
+    gap[k] = !rotated ? half_rest : a.interleaved ? kV : a.half;
+    turn[k] = rotated ? u * kV : -1;
+    token[k] = t;
+    const T* src = reinterpret_cast<const T*>(is_q[k] ? a.q : is_v ? a.v : a.k) +
+                   (is_q[k] ? (token0 + t) * a.q_token_stride + h * a.q_head_stride : (token0 + t) * a.kv_token_stride + h * a.kv_head_stride) + at;
+    to[k] = is_q[k] ? h * a.d + at : (2 * h + (is_v ? 1 : 0)) * a.pg.page_tokens * a.d + at;
+    x[k] = ld_once(src);
+    y[k] = ld_once(src + gap[k]);
+  }
+  if (a.cu_seqlens != nullptr) {   // the sequence of the block's first row: as many as end at it or before
+    int seq = 0;
+    for (int j = 0; j < a.batch; j += kApThreads) seq += __syncthreads_count(j + tid < a.batch && a.cu_seqlens[j + tid + 1] <= token0);
+    if (tid < n_tokens) places[tid] = append_place(a, token0 + tid, seq);
+  } else if (tid < n_tokens) {
+    places[tid] = append_place(a, token0 + tid, token0 + tid);
+  }
+  __syncthreads();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // this block has read the lengths
+  if (alone) {   // nobody else reads them
+    if (a.cu_seqlens == nullptr) {
+      if (tid < n_tokens) advance_window(a, token0 + tid);
+    } else {
+      for (int b = tid; b < a.batch; b += kApThreads) advance_window(a, b);
+    }
+  }
+  for (int i = tid; i < n_tokens * a.half; i += kApThreads) {
+    const int t = i / a.half, u = i - t * a.half;
+    const AppendPlace p = places[t];
+    if (p.seq < a.batch) cs[t][u] = rotary((int64_t)p.place + (a.offsets != nullptr ? a.offsets[p.seq] : 0), a.frequencies[u]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kApItems; ++k) {
+    if (token[k] < 0) continue;
+    const AppendPlace p = places[token[k]];
+    if (p.seq >= a.batch || (!is_q[k] && p.at < 0)) continue;
+    if (turn[k] >= 0) {
+      const float2* c = &cs[token[k]][turn[k]];
+      if (a.interleaved) {
+        x[k] = turn_neighbours<T>(x[k], c);
+        y[k] = turn_neighbours<T>(y[k], c + kV / 2);
+      } else {
+        turn_halves<T>(x[k], y[k], c);
+      }
+    }
+    T* dst = is_q[k] ? reinterpret_cast<T*>(a.q_out) + (int64_t)(token0 + token[k]) * a.n_q_heads * a.d + to[k]
+                     : reinterpret_cast<T*>(a.pool) + p.at + to[k];
+    *reinterpret_cast<uint4*>(dst) = x[k];
+    *reinterpret_cast<uint4*>(dst + gap[k]) = y[k];
+  }
+}
+
+template <class T>
+static int32_t launch_append_as(const AppendArgs& a, cudaStream_t stream) {
+  constexpr int kV = 16 / sizeof(T);
+  const int heads = a.n_q_heads + 2 * a.n_kv_heads;
+  bool advanced = false;
+  auto on16 = [](const void* p, int64_t s0, int64_t s1) { return ((uintptr_t)p & 15) == 0 && s0 * (int64_t)sizeof(T) % 16 == 0 && s1 * (int64_t)sizeof(T) % 16 == 0; };
+  const bool pieces = a.half % kV == 0 && (int64_t)2 * a.n_kv_heads * a.pg.page_tokens * a.d < (1ll << 31) && on16(a.k, a.kv_token_stride, a.kv_head_stride) && on16(a.v, 0, 0) &&
+                      on16(a.q, a.q_token_stride, a.q_head_stride) && on16(a.q_out, 0, 0);
+  if (a.total_tokens > 0 && pieces) {
+    const int64_t per_token = (int64_t)heads * a.d / (2 * kV), most = kApThreads * kApItems;
+    const int slices = (int)((per_token + most - 1) / most);
+    const int tokens = (int)(slices > 1 ? 1 : std::min<int64_t>(kApTokens, most / per_token));
+    const dim3 grid((unsigned)(((int64_t)a.total_tokens + tokens - 1) / tokens * slices));
+    // every row's length is read by one block only, and either no other block's rows belong to the same sequence or there is no other
+    const bool alone = slices == 1 && (a.cu_seqlens == nullptr || grid.x == 1);
+    const int32_t st = launch_dependent(append_window_pieces_kernel<T>, grid, kApThreads, 0, stream, a, tokens, slices, alone);
+    if (st != PQ_OK) return st;
+    advanced = alone;
+  } else if (a.total_tokens > 0) {
+    const int64_t work = (int64_t)a.total_tokens * heads * (a.d / 2);
+    const int32_t st = launch_dependent(append_window_kernel<T>, dim3((unsigned)((work + 255) / 256)), 256, 0, stream, a);
+    if (st != PQ_OK) return st;
+  } else {
+    return PQ_OK;
+  }
+  return advanced ? PQ_OK : launch_dependent(advance_windows_kernel, dim3((unsigned)((a.batch + 127) / 128)), 128, 0, stream, a);
+}
 
 static int32_t launch_append(const AppendArgs& a, int dtype, cudaStream_t stream) {
-  const int64_t work = (int64_t)a.total_tokens * (a.n_q_heads + 2 * a.n_kv_heads) * (a.d / 2);
-  if (work > 0) {
-    const dim3 grid((unsigned)((work + 255) / 256));
-    const int32_t st = dtype == PQ_DTYPE_BF16 ? launch_dependent(append_window_kernel<__nv_bfloat16>, grid, 256, 0, stream, a)
-                                              : launch_dependent(append_window_kernel<float>, grid, 256, 0, stream, a);
-    if (st != PQ_OK) return st;
-  }
-  return launch_dependent(advance_windows_kernel, dim3((unsigned)((a.batch + 127) / 128)), 128, 0, stream, a);
+  return dtype == PQ_DTYPE_BF16 ? launch_append_as<__nv_bfloat16>(a, stream) : launch_append_as<float>(a, stream);
 }
 
 }  // namespace pq
