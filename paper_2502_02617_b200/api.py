@@ -187,19 +187,25 @@ def _on(stream, device):
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, device))
 
 
+def _new_like(q, stream, device):
+    """An uninitialised contiguous tensor of q's shape that belongs to `stream` (None: the current one)."""
+    if stream is None:
+        return torch.empty_like(q, memory_format=torch.contiguous_format)
+    with _on(stream, device):
+        return torch.empty_like(q, memory_format=torch.contiguous_format)
+
+
 def _stream_workspace(kept: dict, need: int, stream, device):
     """At least `need` bytes that belong to `stream` (None: the device's current one): calls on different streams may overlap, so each
-    has its own.  A capture has one too, from the graph's pool: calls outside must not share it with a replay."""
-    if stream is None and device.type == "cuda":
-        stream = torch.cuda.current_stream(device)
-    key = (stream.cuda_stream, torch.cuda.is_current_stream_capturing())
+    has its own.  A capture takes a new one from the graph's pool every time: calls outside must not share it with a replay."""
+    key = (_native or native()).current_stream(device.index) if stream is None else stream.cuda_stream
     ws = kept.get(key)
-    if ws is None or ws.numel() < need or key[1]:
-        while len(kept) >= 8 and key not in kept:   # of streams that are no longer used
-            kept.pop(next(iter(kept)))
+    if ws is None or ws.numel() < need or torch.cuda.is_current_stream_capturing():
         with _on(stream, device):
             ws = torch.empty(need, dtype=torch.uint8, device=device)
-        if not key[1]:
+        if not torch.cuda.is_current_stream_capturing():
+            while len(kept) >= 8 and key not in kept:   # of streams that are no longer used
+                kept.pop(next(iter(kept)))
             kept[key] = ws
     return ws
 
@@ -561,14 +567,13 @@ class PolarQuantCache:
         need = self._shared_need.get(args)
         if need is None:
             need = self._shared_need[args] = size(self.d, *args)
-        return _stream_workspace(self._shared_ws, need, stream, self.device)
+        return _stream_workspace(self._shared_ws, need, stream, self.cache.device)
 
     def attend_prefix(self, q, seq=0, out=None, scale=None, max_len=None, lse=None, stream=None):
         """q [B, Hq, d] or [B, n_q, Hq, d] of any batch: every query attends to all tokens of sequence `seq` of this cache, which
         are decoded once for all (a prompt that many sequences share).  lse: float32 [B, (n_q,) Hq] to write the log-sum-exps to."""
         if out is None:
-            with _on(stream, self.device):
-                out = torch.empty_like(q)
+            out = _new_like(q, stream, self.device)
         most = self.capacity if max_len is None else max_len
         ws = self._shared_workspace(stream, pq_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
         pq_prefix_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
@@ -579,8 +584,7 @@ class PolarQuantCache:
         """q [B, Hq, d], or [B, n_q, Hq, d] for the last n_q positions of every sequence: attention over the shared prefix (sequence `seq`
         of this cache) followed by the sequence's own tokens in `window` (a PagedWindow of B sequences), causal in the window."""
         if out is None:
-            with _on(stream, self.device):
-                out = torch.empty_like(q)
+            out = _new_like(q, stream, self.device)
         most, most_window = self.capacity if max_len is None else max_len, window.capacity if max_window is None else max_window
         ws = self._shared_workspace(stream, pq_shared_workspace_bytes, q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2], self.n_kv_heads,
                                     most, most_window)
@@ -684,7 +688,7 @@ class PagedWindow:
         pq_window_bytes(d, n_kv_heads, page_tokens, n_pages, dtype)   # refuses what the kernels do not take
         self.batch, self.n_q_heads, self.n_kv_heads, self.d = batch, n_q_heads, n_kv_heads, d
         self.page_tokens, self.n_pages, self.interleaved = page_tokens, n_pages, bool(interleaved)
-        self.device = torch.device(device)
+        self.device = torch.empty(0, device=device).device   # with its index
         self.page_table = page_table.to(torch.int32).to(self.device).contiguous()
         assert self.page_table.dim() == 2 and self.page_table.shape[0] == batch
         self.capacity = page_tokens * self.page_table.shape[1]
@@ -693,6 +697,7 @@ class PagedWindow:
         self.lens = torch.zeros(batch, dtype=torch.int32, device=self.device)
         self.status = torch.zeros(STATUS_WORDS, dtype=torch.int32, device=self.device)
         self._ws, self._need = {}, {}   # workspaces by stream, bytes by (queries, max_len)
+        self._unused = torch.empty(16, dtype=torch.uint8, device=self.device)
 
     def _paging_args(self):
         return self.page_table, self.page_tokens, self.n_pages
@@ -701,8 +706,7 @@ class PagedWindow:
         """New rows of every sequence: q [total, Hq, d] (or None), k, v [total, Hkv, d], of which cu_seqlens[b] .. cu_seqlens[b + 1] - 1
         are sequence b's (None: one each); token w of the window has position offsets[b] + w.  Returns the rotated queries."""
         if q is not None and q_out is None:
-            with _on(stream, self.device):
-                q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = _new_like(q, stream, self.device)
         pq_append_window(q, k, v, cu_seqlens, self.frequencies, self.interleaved, offsets, q_out, self.pool, self.lens, self.status,
                          self._paging_args(), stream)
         return q_out
@@ -711,14 +715,15 @@ class PagedWindow:
         need = self._need.get((n_q, max_len))
         if need is None:
             need = self._need[n_q, max_len] = pq_window_workspace_bytes(self.d, self.batch, n_q, self.n_q_heads, self.n_kv_heads, max_len)
+        if need <= self._unused.numel():   # one part: nothing is written
+            return self._unused
         return _stream_workspace(self._ws, need, stream, self.device)
 
     def attend(self, q, out=None, scale=None, max_len=None, lse=None, stream=None):
         """q [B, Hq, d], or [B, n_q, Hq, d] for the last n_q positions of every window (causal).  max_len: a bound on the lengths.
         lse: float32 [B, (n_q,) Hq] to write the log-sum-exps to."""
         if out is None:
-            with _on(stream, self.device):
-                out = torch.empty_like(q)
+            out = _new_like(q, stream, self.device)
         most = self.capacity if max_len is None else max_len
         pq_window_attention(q, self.pool, self.lens, most, self.d ** -0.5 if scale is None else scale, out, lse,
                             self._workspace(q.shape[1] if q.dim() == 4 else 1, most, stream), self.status, self._paging_args(), stream)

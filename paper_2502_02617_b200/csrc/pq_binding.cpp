@@ -429,7 +429,21 @@ PyObject* shared_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// current_stream(device index): the handle of PyTorch's current stream there
+PyObject* current_stream(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  try {
+    check(n == 1, "expected a device index");
+    return PyLong_FromVoidPtr(c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)i32(a[0])).stream());
+  } catch (const PyError&) {
+    return nullptr;
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+  }
+}
+
 PyMethodDef kMethods[] = {
+    {"current_stream", (PyCFunction)(void (*)(void))current_stream, METH_FASTCALL, nullptr},
     {"prefix_attend", (PyCFunction)(void (*)(void))prefix_attend, METH_FASTCALL, nullptr},
     {"shared_attend", (PyCFunction)(void (*)(void))shared_attend, METH_FASTCALL, nullptr},
     {"append_window", (PyCFunction)(void (*)(void))append_window, METH_FASTCALL, nullptr},

@@ -35,6 +35,12 @@ __device__ __forceinline__ float win_exp2(float x) { return exp2f(x); }
 // exp2 of a difference of references: 0 from -inf on, 1 where nothing changes (also from -inf to -inf)
 __device__ __forceinline__ float win_rescale(float from, float to) { return from == to ? 1.f : win_exp2(from - to); }
 
+__device__ __forceinline__ float2 cluster_ld2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr));
+  return v;
+}
+
 template <class T, int D, int kRows_>
 struct WindowShape {
   static constexpr int kRows = kRows_;
@@ -68,6 +74,63 @@ __device__ __forceinline__ void win_pairs(uint4 w, uint64_t* x) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) x[i] = f2_pack(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
   }
+}
+
+// The last step of a block: the blocks of the cluster merge their outputs y [n_rows][D], relative to (reference, denominator) bl, each
+// block a share of the elements, and store them.
+template <int D, class RowOf, class Seen>
+__device__ __forceinline__ void window_finish(const WindowArgs& a, const float* y, const float2* bl, int n_rows, RowOf row_of, Seen seen) {
+  uint32_t rank, n_blocks;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
+  cluster_arrive();
+  cluster_wait();
+  const uint32_t y_at = (uint32_t)__cvta_generic_to_shared(y), bl_at = (uint32_t)__cvta_generic_to_shared(bl);
+  const int part = blockIdx.x / n_blocks;
+  for (int i = threadIdx.x + kWinThreads * rank; i < n_rows * D / 4; i += kWinThreads * n_blocks) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    float2 ml[kWinMaxCluster];
+    float4 v[kWinMaxCluster];
+#pragma unroll
+    for (uint32_t k = 0; k < kWinMaxCluster; ++k) {   // all in flight at once
+      ml[k] = make_float2(-CUDART_INF_F, 0.f);
+      v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k < n_blocks) {
+        ml[k] = cluster_ld2(cluster_map(bl_at + r * 8, k));
+        v[k] = cluster_ld4(cluster_map(y_at + (r * D + c) * 4, k));
+      }
+    }
+    float M = -CUDART_INF_F, L = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kWinMaxCluster; ++k) M = fmaxf(M, ml[k].x);
+#pragma unroll
+    for (int k = 0; k < kWinMaxCluster; ++k) {   // block order: the result does not depend on who asks
+      const float w = win_rescale(ml[k].x, M);
+      L = fmaf(ml[k].y, w, L);
+      acc = make_float4(fmaf(v[k].x, w, acc.x), fmaf(v[k].y, w, acc.y), fmaf(v[k].z, w, acc.z), fmaf(v[k].w, w, acc.w));
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;   // nothing seen, or only scores of -inf: zeros
+    acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    const int64_t row = row_of(r), at = row * D + c;
+    const float lse = L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f;
+    if (a.n_parts > 1) {
+      *reinterpret_cast<float4*>(a.part_out + part * a.n_rows * D + at) = acc;
+      if (c == 0) a.part_lse[part * a.n_rows + row] = lse;
+    } else {
+      if (a.out_dtype == PQ_DTYPE_BF16) {
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
+        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+        *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = acc;
+      }
+      if (c == 0 && a.lse != nullptr) a.lse[row] = lse;
+    }
+    if (c == 0 && a.lse == nullptr && part == 0 && seen(r) == 0) set_status(a.status, PQ_ERR_EMPTY);
+  }
+  cluster_arrive();   // nobody leaves while its shared memory may be read
+  cluster_wait();
 }
 
 // Sums of kN values over 2 kOff lanes: every exchange halves the values that a lane holds.
@@ -322,47 +385,7 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
     *reinterpret_cast<float4*>(&y_sm[r][c]) = acc;
     if (c == 0) bl_sm[r] = make_float2(M, L);
   }
-  // ---- the blocks of the cluster: each takes a share of the output's elements
-  uint32_t rank, n_blocks;
-  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
-  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
-  cluster_arrive();
-  cluster_wait();
-  const uint32_t y_at = (uint32_t)__cvta_generic_to_shared(&y_sm[0][0]), bl_at = (uint32_t)__cvta_generic_to_shared(&bl_sm[0]);
-  const int part = blockIdx.x / n_blocks;
-  for (int i = tid + kWinThreads * rank; i < n_rows * D / 4; i += kWinThreads * n_blocks) {
-    const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    float M = -CUDART_INF_F, L = 0.f;
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (uint32_t k = 0; k < n_blocks; ++k) {   // block order: the result does not depend on who asks
-      const float2 ml = make_float2(cluster_ld(cluster_map(bl_at + r * 8, k)), cluster_ld(cluster_map(bl_at + r * 8 + 4, k)));
-      const float4 v = cluster_ld4(cluster_map(y_at + (r * D + c) * 4, k));
-      const float m_new = fmaxf(M, ml.x), was = win_rescale(M, m_new), is = win_rescale(ml.x, m_new);
-      M = m_new;
-      L = L * was + ml.y * is;
-      acc = make_float4(acc.x * was + v.x * is, acc.y * was + v.y * is, acc.z * was + v.z * is, acc.w * was + v.w * is);
-    }
-    const float inv = L == 0.f ? 0.f : 1.f / L;   // nothing seen, or only scores of -inf: zeros
-    acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-    const int64_t row = row_of(r), at = row * D + c;
-    const float lse = L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f;
-    if (a.n_parts > 1) {
-      *reinterpret_cast<float4*>(a.part_out + part * a.n_rows * D + at) = acc;
-      if (c == 0) a.part_lse[part * a.n_rows + row] = lse;
-    } else {
-      if (a.out_dtype == PQ_DTYPE_BF16) {
-        const __nv_bfloat162 lo = __floats2bfloat162_rn(acc.x, acc.y), hi = __floats2bfloat162_rn(acc.z, acc.w);
-        *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out) + at) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-      } else {
-        *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out) + at) = acc;
-      }
-      if (c == 0 && a.lse != nullptr) a.lse[row] = lse;
-    }
-    if (c == 0 && a.lse == nullptr && part == 0 && seen(r) == 0) set_status(a.status, PQ_ERR_EMPTY);
-  }
-  cluster_arrive();   // nobody leaves while its shared memory may be read
-  cluster_wait();
+  window_finish<D>(a, &y_sm[0][0], bl_sm, n_rows, row_of, seen);
 }
 
 // How a window's tokens are cut: clusters of up to eight blocks, and parts beyond that.  Two blocks' worth of work for each of the
@@ -379,11 +402,11 @@ static WindowCut cut_window(int64_t units, int max_len, int n_sm) {
   return c;
 }
 
-template <class T, int D, int kRows>
-static int32_t launch_window_as(WindowArgs a, int batch, const WindowCut& cut, cudaStream_t stream) {
+static int32_t launch_window(void (*kernel)(WindowArgs), const WindowArgs& a, int batch, const WindowCut& cut, int smem, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(cut.cluster * cut.parts, a.n_kv_heads * a.row_blocks, batch);
   cfg.blockDim = dim3(kWinThreads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -394,7 +417,7 @@ static int32_t launch_window_as(WindowArgs a, int batch, const WindowCut& cut, c
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, window_attention_kernel<T, D, kRows>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
   if (e != cudaSuccess) {
     note_cuda_error(e);
     cudaGetLastError();
@@ -404,9 +427,8 @@ static int32_t launch_window_as(WindowArgs a, int batch, const WindowCut& cut, c
 }
 template <class T, int D>
 static int32_t launch_window_rows(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
-  return rows == 1   ? launch_window_as<T, D, 1>(a, batch, cut, stream)
-         : rows == 2 ? launch_window_as<T, D, 2>(a, batch, cut, stream)
-                     : launch_window_as<T, D, 4>(a, batch, cut, stream);
+  return launch_window(rows == 1 ? window_attention_kernel<T, D, 1> : rows == 2 ? window_attention_kernel<T, D, 2> : window_attention_kernel<T, D, 4>, a, batch,
+                       cut, 0, stream);
 }
 template <class T>
 static int32_t launch_window_dim(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
@@ -417,11 +439,4 @@ static int32_t launch_window_dim(const WindowArgs& a, int rows, int batch, const
     default: return launch_window_rows<T, 128>(a, rows, batch, cut, stream);
   }
 }
-// (query, head) rows of a block for `all` rows of a kv head.
-static int window_block_rows(int64_t all) { return all == 1 ? 1 : all == 2 ? 2 : 4; }
-static int64_t window_row_blocks(int n_q, int g) {
-  const int64_t all = (int64_t)n_q * g;
-  return (all + window_block_rows(all) - 1) / window_block_rows(all);
-}
-
 }  // namespace pq
