@@ -1192,10 +1192,8 @@ int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, 
   if (batch <= 0 || n_q <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_len <= 0 || n_q_heads % n_kv_heads) return PQ_ERR_INVALID_ARG;
   const int64_t rows = (int64_t)batch * n_q * n_q_heads;
   int64_t parts = 1;   // of the kernel that cuts more
-  for (int32_t dtype : {PQ_DTYPE_F32, PQ_DTYPE_BF16}) {
-    const int64_t units = (int64_t)batch * n_kv_heads * pq::window_row_blocks(head_dim, dtype, n_q, n_q_heads / n_kv_heads);
-    parts = std::max<int64_t>(parts, pq::cut_window(units, max_len, pq::kFastMaxGridHost).parts);
-  }
+  for (int32_t dtype : {PQ_DTYPE_F32, PQ_DTYPE_BF16})
+    parts = std::max<int64_t>(parts, pq::window_cut(head_dim, dtype, batch, n_q, n_kv_heads, n_q_heads / n_kv_heads, max_len, pq::kFastMaxGridHost).parts);
   return parts > 1 ? parts * rows * (head_dim + 1) * 4 : 16;
 }
 
@@ -1214,20 +1212,20 @@ static int32_t window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   if (((uintptr_t)q_dev | (uintptr_t)pool_dev | (uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
   if (((uintptr_t)window_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
   const int g = n_q_heads / n_kv_heads;
-  const int64_t row_blocks = pq::window_row_blocks(head_dim, kv_dtype, n_q, g);
-  if (batch > 65535 || n_kv_heads * row_blocks > 65535) return PQ_ERR_UNSUPPORTED;
+  const pq::WindowRows rows = pq::window_rows(head_dim, kv_dtype, n_q, g);
+  if (batch > 65535 || n_kv_heads * rows.blocks > 65535) return PQ_ERR_UNSUPPORTED;
   if (only_check) return PQ_OK;
   static pq::DeviceMemo sm_count;
   const int n_sm = pq::sm_count_of_device(sm_count);
   if (n_sm == 0) return PQ_ERR_CUDA;
-  const pq::WindowCut cut = pq::cut_window(batch * n_kv_heads * row_blocks, max_len, std::min(n_sm, pq::kFastMaxGridHost));
+  const pq::WindowCut cut = pq::window_cut(head_dim, kv_dtype, batch, n_q, n_kv_heads, g, max_len, std::min(n_sm, pq::kFastMaxGridHost));
   a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype;
-  a.row_blocks = (int)row_blocks; a.n_parts = cut.parts; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
+  a.row_blocks = (int)rows.blocks; a.n_parts = cut.parts; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
   a.q = q_dev; a.pool = reinterpret_cast<const uint8_t*>(pool_dev); a.lens = window_lens_dev; a.out = out_dev; a.lse = lse_dev;
   a.part_out = reinterpret_cast<float*>(workspace_dev); a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * head_dim : 0);
   a.status = status_dev;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  st = pq::launch_window_attention(a, kv_dtype, pq::window_block_rows(head_dim, kv_dtype, (int64_t)n_q * g), batch, cut, s);
+  st = pq::launch_window_attention(a, kv_dtype, rows.rows, batch, cut, s);
   if (st != PQ_OK || cut.parts == 1) return st;
   // the window kernel has reported the rows that see nothing
   return pq::launch_merge(head_dim, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, out_dev, out_dtype, lse_dev, nullptr, s);

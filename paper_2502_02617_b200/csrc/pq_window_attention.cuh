@@ -7,8 +7,8 @@
 // halves the values with every step (kVals values over kLanes lanes cost kVals - 1 shuffles, and each lane ends with one
 // score).  The streams meet at the end: groups by shuffles, warps in shared memory, the blocks of a cluster in each other's
 // shared memory, and the parts beyond a cluster in merge_attention_kernel.  Everything is float32 on the values as they are.
-// Bound by HBM: a token is 2 head_dim elements, about 22 cycles of an SM's share at head_dim 128 in bf16, and 4 rows take
-// about 11 cycles of issue.
+// bf16 rows of 64 and 128 are faster on tensor cores (pq_window_mma.cuh).  Bound by issue and the latency of its loads: 16 sequences of 2000
+// float32 tokens, 32/8 heads of 128, 56 us (4.7 TB/s); in bf16, 64 of up to 4096 tokens, it took 193 us against 111 there.
 #pragma once
 
 #include "pq_window_common.cuh"
@@ -388,17 +388,21 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
   window_finish<D>(a, &y_sm[0][0], bl_sm, n_rows, row_of, seen);
 }
 
-// How a window's tokens are cut: clusters of up to eight blocks, and parts beyond that.  Two blocks' worth of work for each of the
-// four that an SM holds, but no block below 128 tokens.
+// How a window's tokens are cut among clusters of up to eight blocks, and parts beyond that.  An SM holds four blocks, and a block costs
+// about 4 us beside its tiles of 16 tokens, of which each of its `streams` takes 0.9 us: one wave of blocks where that leaves a block two
+// tiles at least, more where a block still has 16 tiles for every stream (uneven lengths then level out), and a merge kernel (2.5 us) only
+// where a stream would have more than eight tiles.  us at 1, 2, 4, 8 splits, 32/8 heads: 16 sequences of 500 tokens 15.2, 13.7, 11.4, 16.8;
+// of 2048 43, 35, 27, 31; 64 of 200 16, 21, 29, 50; 64 of 1024 to 4096 129, 119, 111, 121; one of 4096 66, 35, 20, 12.4 and in eight parts 11.1.
 struct WindowCut {
   int cluster, parts;
 };
-static WindowCut cut_window(int64_t units, int max_len, int n_sm) {
-  const int64_t want = (8 * (int64_t)n_sm + units - 1) / units, most = ((int64_t)max_len + 127) / 128;
-  const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+static WindowCut cut_window(int64_t units, int max_len, int n_sm, int streams) {
+  const int64_t tiles = ((int64_t)max_len + 15) / 16, one_wave = std::max<int64_t>(1, 4 * (int64_t)n_sm / units);
+  const int64_t splits = std::min(std::max<int64_t>(1, tiles / 2), std::max(one_wave, tiles / (16 * streams)));
   WindowCut c = {1, 1};
   while (c.cluster < kWinMaxCluster && 2 * c.cluster <= splits) c.cluster *= 2;
-  if (c.cluster == kWinMaxCluster) c.parts = (int)std::min<int64_t>(kWinMaxParts, splits / kWinMaxCluster);
+  if (c.cluster == kWinMaxCluster)
+    c.parts = (int)std::max<int64_t>(1, std::min({(tiles + 64 * streams - 1) / (64 * streams), one_wave / kWinMaxCluster, (int64_t)kWinMaxParts}));
   return c;
 }
 
@@ -429,14 +433,5 @@ template <class T, int D>
 static int32_t launch_window_rows(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
   return launch_window(rows == 1 ? window_attention_kernel<T, D, 1> : rows == 2 ? window_attention_kernel<T, D, 2> : window_attention_kernel<T, D, 4>, a, batch,
                        cut, 0, stream);
-}
-template <class T>
-static int32_t launch_window_dim(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
-  switch (a.d) {
-    case 16: return launch_window_rows<T, 16>(a, rows, batch, cut, stream);
-    case 32: return launch_window_rows<T, 32>(a, rows, batch, cut, stream);
-    case 64: return launch_window_rows<T, 64>(a, rows, batch, cut, stream);
-    default: return launch_window_rows<T, 128>(a, rows, batch, cut, stream);
-  }
 }
 }  // namespace pq

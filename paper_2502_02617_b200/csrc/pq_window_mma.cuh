@@ -8,19 +8,22 @@
 // Products of bf16 are exact in float32 and summed there; scale and softmax are float32.
 // A weight or term of 0 times an infinite value or key is a NaN that the row itself may not see: a block whose result holds a NaN
 // is computed again, row by row, by window_again.
+// Bound by HBM where there is enough of a window: 64 sequences of 1024 to 4096 tokens, 32/8 heads of 128, 713 MB in 111 us (6.4 TB/s); 16 of
+// 2048 in 27 us.  Four blocks on an SM: with the query fragments in registers (166) and a ring of four pieces three fitted, and 64 sequences
+// of 200 tokens took 22 us instead of 16.
 #pragma once
 
 namespace pq {
 
-constexpr int kWmTile = 16, kWmRing = 4;
+constexpr int kWmTile = 16, kWmRing = 3;
 template <int D, int kQTerms, int kTiles>
 struct WmShape {
   static constexpr int kStreams = kWinWarps / kTiles, kRows = 16 * kTiles;
   static constexpr int kPiece = kWmTile * D * 2, kRingBytes = kStreams * kWmRing * kPiece;
   static constexpr int kOut = kStreams * kRows * D * 4;        // the streams' outputs, where the ring was
   static constexpr int kMl = kRingBytes > kOut ? kRingBytes : kOut;   // (reference, denominator) [stream][row]
-  static constexpr int kQ = kMl + kStreams * kRows * 8;        // float32 queries: fragments [tile][term][k-step][lane]
-  static constexpr int kBytes = kQ + (kQTerms > 1 ? kTiles * kQTerms * (D / 16) * 512 : 0);
+  static constexpr int kQ = kMl + kStreams * kRows * 8;        // queries: fragments [tile][term][k-step][lane]
+  static constexpr int kBytes = kQ + kTiles * kQTerms * (D / 16) * 512;
 };
 
 // The rows of a block in float32, a warp at a time, whatever the values: y [rows][D] and ml as window_finish takes them.
@@ -63,7 +66,7 @@ __device__ __noinline__ void window_again(const WindowArgs& a, int b, int hk, in
 }
 
 template <int D, int kQTerms, int kTiles>
-__global__ void __launch_bounds__(kWinThreads) window_mma_kernel(const __grid_constant__ WindowArgs a) {
+__global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid_constant__ WindowArgs a) {
   using W = WmShape<D, kQTerms, kTiles>;
   constexpr int kSteps = D / 16, kChunks = D / 8, kThreads = 32 * kTiles;   // threads of a stream
   extern __shared__ __align__(128) uint8_t wm_smem[];
@@ -140,29 +143,23 @@ __global__ void __launch_bounds__(kWinThreads) window_mma_kernel(const __grid_co
   for (int i = 0; i < kWmRing; ++i) request(i);
 
   // ---- queries: A operand of row g8 and g8 + 8 of the warp's tile (rows past the last repeat it)
-  uint32_t q[kSteps][4];
-  const int64_t row_lo = row_of(min(16 * tile + g8, n_rows - 1)) * D, row_hi = row_of(min(16 * tile + g8 + 8, n_rows - 1)) * D;
   uint4* q_sm = reinterpret_cast<uint4*>(wm_smem + W::kQ) + tile * (kQTerms * kSteps * 32) + lane;
-  if constexpr (kQTerms == 1) {
-    const __nv_bfloat16* qp = reinterpret_cast<const __nv_bfloat16*>(a.q);
+  {
+    const int64_t row_lo = row_of(min(16 * tile + g8, n_rows - 1)) * D, row_hi = row_of(min(16 * tile + g8 + 8, n_rows - 1)) * D;
 #pragma unroll
-    for (int ks = 0; ks < kSteps; ++ks) {
-      const int k = 16 * ks + 2 * c4;
-      q[ks][0] = *reinterpret_cast<const uint32_t*>(qp + row_lo + k);
-      q[ks][1] = *reinterpret_cast<const uint32_t*>(qp + row_hi + k);
-      q[ks][2] = *reinterpret_cast<const uint32_t*>(qp + row_lo + k + 8);
-      q[ks][3] = *reinterpret_cast<const uint32_t*>(qp + row_hi + k + 8);
-    }
-  } else {
-    if (stream == 0) {
-      const float* qp = reinterpret_cast<const float*>(a.q);
-#pragma unroll 1
-      for (int ks = 0; ks < kSteps; ++ks) {
+    for (int i = 0; i < kSteps / W::kStreams; ++i) {   // the streams share the work
+      const int ks = stream + i * W::kStreams, k = 16 * ks + 2 * c4;
+      if constexpr (kQTerms == 1) {
+        const __nv_bfloat16* qp = reinterpret_cast<const __nv_bfloat16*>(a.q) + k;
+        q_sm[ks * 32] = make_uint4(*reinterpret_cast<const uint32_t*>(qp + row_lo), *reinterpret_cast<const uint32_t*>(qp + row_hi),
+                                   *reinterpret_cast<const uint32_t*>(qp + row_lo + 8), *reinterpret_cast<const uint32_t*>(qp + row_hi + 8));
+      } else {
+        const float* qp = reinterpret_cast<const float*>(a.q) + k;
         uint32_t w[4][3];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 v = *reinterpret_cast<const float2*>(qp + ((i & 1) ? row_hi : row_lo) + 16 * ks + 2 * c4 + 8 * (i >> 1));
-          bf16_terms(v.x, v.y, w[i]);
+        for (int e = 0; e < 4; ++e) {
+          const float2 v = *reinterpret_cast<const float2*>(qp + ((e & 1) ? row_hi : row_lo) + 8 * (e >> 1));
+          bf16_terms(v.x, v.y, w[e]);
         }
 #pragma unroll
         for (int term = 0; term < 3; ++term) q_sm[(term * kSteps + ks) * 32] = make_uint4(w[0][term], w[1][term], w[2][term], w[3][term]);
@@ -190,17 +187,12 @@ __global__ void __launch_bounds__(kWinThreads) window_mma_kernel(const __grid_co
       for (int ks = 0; ks < kSteps; ++ks) {
         uint32_t k4[4];
         ldmatrix_x4<false>(at + (((2 * ks + k_half) ^ (k_row & 7)) << 4), k4);
-        if constexpr (kQTerms == 1) {
-          mma_bf16_16816(s[0], q[ks], k4[0], k4[1]);
-          mma_bf16_16816(s[1], q[ks], k4[2], k4[3]);
-        } else {
 #pragma unroll
-          for (int term = kQTerms - 1; term >= 0; --term) {
-            const uint4 w = q_sm[(term * kSteps + ks) * 32];
-            const uint32_t qa[4] = {w.x, w.y, w.z, w.w};
-            mma_bf16_16816(s[0], qa, k4[0], k4[1]);
-            mma_bf16_16816(s[1], qa, k4[2], k4[3]);
-          }
+        for (int term = kQTerms - 1; term >= 0; --term) {   // small terms first
+          const uint4 w = q_sm[(term * kSteps + ks) * 32];
+          const uint32_t qa[4] = {w.x, w.y, w.z, w.w};
+          mma_bf16_16816(s[0], qa, k4[0], k4[1]);
+          mma_bf16_16816(s[1], qa, k4[2], k4[3]);
         }
       }
     }
@@ -330,22 +322,43 @@ static int32_t launch_window_mma_rows(const WindowArgs& a, int rows, int batch, 
                       : launch_window_mma_as<D, kQTerms, 4>(a, batch, cut, stream);
 }
 
-// Which kernel takes a call, and the (query, head) rows of its blocks for `all` rows of a kv head.
+// Which kernel takes a call, the (query, head) rows of its blocks for `all` rows of a kv head, and the streams of tokens in a block.
 static bool window_on_tensor_cores(int d, int kv_dtype) { return kv_dtype == PQ_DTYPE_BF16 && d >= 64; }
-static int window_block_rows(int d, int kv_dtype, int64_t all) {
-  if (window_on_tensor_cores(d, kv_dtype)) return all <= 16 ? 16 : all <= 32 ? 32 : 64;
-  return all == 1 ? 1 : all == 2 ? 2 : 4;
+struct WindowRows {
+  int rows, streams;
+  int64_t blocks;
+};
+static WindowRows window_rows(int d, int kv_dtype, int n_q, int g) {
+  const int64_t all = (int64_t)n_q * g;
+  WindowRows r;
+  if (window_on_tensor_cores(d, kv_dtype)) {
+    r.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
+    r.streams = 64 / r.rows;
+  } else {
+    r.rows = all == 1 ? 1 : all == 2 ? 2 : 4;
+    r.streams = kWinWarps;
+  }
+  r.blocks = (all + r.rows - 1) / r.rows;
+  return r;
 }
-static int64_t window_row_blocks(int d, int kv_dtype, int n_q, int g) {
-  const int64_t all = (int64_t)n_q * g, rows = window_block_rows(d, kv_dtype, all);
-  return (all + rows - 1) / rows;
+static WindowCut window_cut(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len, int n_sm) {
+  const WindowRows r = window_rows(d, kv_dtype, n_q, g);
+  return cut_window(batch * n_kv_heads * r.blocks, max_len, n_sm, r.streams);
 }
 static int32_t launch_window_attention(const WindowArgs& a, int kv_dtype, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
-  if (!window_on_tensor_cores(a.d, kv_dtype))
-    return kv_dtype == PQ_DTYPE_BF16 ? launch_window_dim<__nv_bfloat16>(a, rows, batch, cut, stream) : launch_window_dim<float>(a, rows, batch, cut, stream);
-  const bool exact = a.io_dtype == PQ_DTYPE_BF16;
-  if (a.d == 64) return exact ? launch_window_mma_rows<64, 1>(a, rows, batch, cut, stream) : launch_window_mma_rows<64, 3>(a, rows, batch, cut, stream);
-  return exact ? launch_window_mma_rows<128, 1>(a, rows, batch, cut, stream) : launch_window_mma_rows<128, 3>(a, rows, batch, cut, stream);
+  const bool exact = a.io_dtype == PQ_DTYPE_BF16;   // queries that are one bf16 term
+  if (window_on_tensor_cores(a.d, kv_dtype)) {
+    if (a.d == 64) return exact ? launch_window_mma_rows<64, 1>(a, rows, batch, cut, stream) : launch_window_mma_rows<64, 3>(a, rows, batch, cut, stream);
+    return exact ? launch_window_mma_rows<128, 1>(a, rows, batch, cut, stream) : launch_window_mma_rows<128, 3>(a, rows, batch, cut, stream);
+  }
+  if (kv_dtype == PQ_DTYPE_BF16)
+    return a.d == 16 ? launch_window_rows<__nv_bfloat16, 16>(a, rows, batch, cut, stream) : launch_window_rows<__nv_bfloat16, 32>(a, rows, batch, cut, stream);
+  switch (a.d) {
+    case 16: return launch_window_rows<float, 16>(a, rows, batch, cut, stream);
+    case 32: return launch_window_rows<float, 32>(a, rows, batch, cut, stream);
+    case 64: return launch_window_rows<float, 64>(a, rows, batch, cut, stream);
+    default: return launch_window_rows<float, 128>(a, rows, batch, cut, stream);
+  }
 }
 
 }  // namespace pq
