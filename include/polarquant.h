@@ -464,7 +464,7 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
  *   cache_lens_dev    int32[cache_batch], the cache's; the queries see the cache_lens[sequence] tokens of `sequence`
  *   max_len           host-side upper bound on that length
  *   lse_dev           float32 [n_queries][n_q_heads] or NULL; with it an empty prefix yields zeros and -inf and is no error
- *   workspace_dev     pq_workspace_bytes(head_dim, n_queries, n_q_heads, n_kv_heads, max_len) bytes
+ *   workspace_dev     pq_prefix_workspace_bytes(...) bytes; as for pq_decode_attention
  * Tolerances are those of pq_multi_query_attention.
  *
  * pq_shared_attention: the last n_q positions of every sequence attend to the shared prefix and, causally, to their own paged
@@ -472,6 +472,7 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
  * partial results are float32 and merged by their log-sum-exps.  A query that sees no token yields zeros and records
  * PQ_ERR_EMPTY.  workspace_dev: pq_shared_workspace_bytes(...) bytes; two calls that overlap in time must not share it.
  */
+int64_t pq_prefix_workspace_bytes(int32_t head_dim, int32_t n_queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len);
 int32_t pq_prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
                             const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
                             const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,

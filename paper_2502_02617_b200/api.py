@@ -75,6 +75,7 @@ _SIGNATURES = {
     "pq_window_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32]),
     "pq_window_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_void_p, c_int32, c_int32,
                                       c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
+    "pq_prefix_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32]),
     "pq_prefix_attention": (c_int32, [c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_void_p, c_int32,
                                       c_int32, c_int32, c_void_p, c_int32, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]),
     "pq_shared_workspace_bytes": (c_int64, [c_int32, c_int32, c_int32, c_int32, c_int32, c_int32, c_int32]),
@@ -426,9 +427,16 @@ def pq_window_attention(q, pool, lens, max_len, scale, out, lse, workspace, stat
     _check((_native or native()).window_attend(q, pool, lens, max_len, scale, out, lse, workspace, status, paging, stream), "pq_window_attention")
 
 
+def pq_prefix_workspace_bytes(d: int, n_queries: int, n_q_heads: int, n_kv_heads: int, max_len: int) -> int:
+    n = int(lib().pq_prefix_workspace_bytes(d, n_queries, n_q_heads, n_kv_heads, max_len))
+    if n < 0:
+        raise PolarQuantError(n, "pq_prefix_workspace_bytes")
+    return n
+
+
 def pq_prefix_attention(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, lse, workspace, status, paging=None, stream=None):
     """Every query of q [..., Hq, d] attends to all tokens of sequence `seq` of a packed cache, decoded once for all.  `workspace` must hold
-    pq_workspace_bytes(d, queries, Hq, Hkv, max_len); `paging`: None, or (page table, tokens per page, pages) for a paged cache."""
+    pq_prefix_workspace_bytes(d, queries, Hq, Hkv, max_len); `paging`: None, or (page table, tokens per page, pages) for a paged cache."""
     _check((_native or native()).prefix_attend(S, tables, q, cache, lens, seq, n_kv_heads, capacity, max_len, scale, out, workspace, status, paging,
                                                stream, lse), "pq_prefix_attention")
 
@@ -575,7 +583,7 @@ class PolarQuantCache:
         if out is None:
             out = _new_like(q, stream, self.device)
         most = self.capacity if max_len is None else max_len
-        ws = self._shared_workspace(stream, pq_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
+        ws = self._shared_workspace(stream, pq_prefix_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
         pq_prefix_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
                             self.d ** -0.5 if scale is None else scale, out, lse, ws, self.status, self._paging_args(), stream)
         return out

@@ -400,7 +400,7 @@ PyObject* prefix_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const at::Tensor* lse = tensor_or_none(a[15]);
     check(lse == nullptr || (lse->scalar_type() == at::kFloat && lse->is_contiguous() && lse->sizes() == p.q.sizes().slice(0, p.q.dim() - 1)),
           "lse must be a contiguous float32 tensor of q's shape without the last dimension");
-    const int64_t need = pq_workspace_bytes(p.d, p.queries(), p.hq, p.hkv, p.max_len);
+    const int64_t need = pq_prefix_workspace_bytes(p.d, p.queries(), p.hq, p.hkv, p.max_len);
     check(need < 0 || (int64_t)p.ws.nbytes() >= need, "the workspace is too small");   // below 0: the call itself says why
     const c10::Device device = one_device({&p.q, &p.S, &p.tables, &p.cache, &p.lens, &p.out, &p.ws, &p.status, lse});
     const c10::cuda::CUDAGuard guard(device);

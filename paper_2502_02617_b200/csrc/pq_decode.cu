@@ -315,12 +315,17 @@ __global__ void __launch_bounds__(256) merge_attention_kernel(int d, int64_t n_r
   if (idx >= n_rows * d) return;
   const int64_t row = idx / d;
   float mx = -CUDART_INF_F;
+  bool nan = false;   // a part that is not a number makes the row one
 #pragma unroll 8
-  for (int p = 0; p < n_parts; ++p) mx = fmaxf(mx, parts_lse[(int64_t)p * n_rows + row]);
+  for (int p = 0; p < n_parts; ++p) {
+    const float l = parts_lse[(int64_t)p * n_rows + row];
+    mx = fmaxf(mx, l);
+    nan = nan || l != l;
+  }
   float acc[kV], wsum = 0.f;
 #pragma unroll
   for (int e = 0; e < kV; ++e) acc[e] = 0.f;
-  if (mx > -CUDART_INF_F) {
+  if (mx > -CUDART_INF_F || nan) {
 #pragma unroll 4
     for (int p = 0; p < n_parts; ++p) {   // part order: the result does not depend on the launch
       const float l = parts_lse[(int64_t)p * n_rows + row];
@@ -364,7 +369,7 @@ __global__ void __launch_bounds__(256) merge_attention_kernel(int d, int64_t n_r
   } else {
     reinterpret_cast<float*>(out)[idx] = acc[0];
   }
-  if (lse_out != nullptr && idx == row * d) lse_out[row] = mx > -CUDART_INF_F ? mx + __logf(wsum) : -CUDART_INF_F;
+  if (lse_out != nullptr && idx == row * d) lse_out[row] = mx > -CUDART_INF_F || nan ? mx + __logf(wsum) : -CUDART_INF_F;
 }
 
 static int32_t launch_merge(int d, int64_t n_rows, int n_parts, const void* parts_out, int parts_dtype, const float* parts_lse, void* out,
@@ -575,6 +580,8 @@ __global__ void __launch_bounds__(kTailThreads) tail_attention_kernel(const __gr
 #include "pq_tail_mma.cuh"
 #include "pq_window_attention.cuh"
 #include "pq_window_mma.cuh"
+#include "pq_prefix.cuh"
+#include "pq_prefix_tc.cuh"
 namespace pq {
 
 // ---- inspection kernels ----------------------------------------------------------------------
@@ -866,7 +873,45 @@ static int32_t launch_prefill_tc(DecodeArgs a, int batch, int n_q, int n_splits,
   }
   const int32_t main_st = launch_status();
   if (main_st != PQ_OK) return main_st;
-  return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.out_dtype, a.lse, a.status, stream);
+  return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.io_dtype, a.status, stream);
+}
+
+// The same for queries that all see the whole sequence: prefix_tc_kernel, and what follows it.
+template <int kCtas>
+static int32_t launch_prefix_tc(DecodeArgs a, const SharedPrefix& shared, int n_splits, cudaStream_t stream) {
+  static DeviceMemo configured;
+  if (configure_for_device(prefix_tc_kernel<kCtas>, kPcSmTotal, configured) == 0) return PQ_ERR_CUDA;
+  const int qb_rows = kPtRows / (a.n_q_heads / a.n_kv_heads), q_blocks = (a.n_q + qb_rows - 1) / qb_rows;
+  a.n_splits = n_splits;
+  const int64_t all_rows = (int64_t)a.batch * a.n_q_heads;   // the workspace: rotated queries, parts, their log-sum-exps
+  __half* qrot = reinterpret_cast<__half*>(a.ws.elected);
+  a.qrot = qrot;
+  a.part_out = reinterpret_cast<float*>(qrot + all_rows * 256);
+  a.part_lse = a.part_out + n_splits * all_rows * 128;
+  const int32_t st = launch_prefix_rotate<128>(a.S, a.q, a.io_dtype, all_rows, a.scale * 1.4426950408889634f, qrot, stream);
+  if (st != PQ_OK) return st;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((q_blocks + kCtas - 1) / kCtas * kCtas, a.n_kv_heads, n_splits);
+  cfg.blockDim = dim3(kPcThreads);
+  cfg.dynamicSmemBytes = kPcSmTotal;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set up while the kernel before it finishes (it waits inside)
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCtas;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tc_kernel<kCtas>, a);
+  if (e != cudaSuccess) {
+    note_cuda_error(e);
+    cudaGetLastError();
+    return PQ_ERR_CUDA;
+  }
+  const int32_t main_st = launch_status();
+  return main_st != PQ_OK ? main_st : finish_prefix<128>(a, shared, a.part_out, a.part_lse, n_splits, stream);
 }
 
 }  // namespace pq
@@ -888,16 +933,20 @@ int64_t pq_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q_heads, i
   return std::max(std::max(cut, one), parts);
 }
 
-// The queries see the whole sequence, and the output may be of another type than they are.
-struct SharedPrefix {
-  int out_dtype;
-};
+// Behind a kernel that has written the prefix's own result (shared->part_out): the window, and the merge of the two.
+static int32_t then_window(int32_t st, const pq::SharedPrefix* shared, int32_t* status, cudaStream_t stream) {
+  if (st != PQ_OK || shared == nullptr || shared->window == nullptr) return st;
+  const pq::WindowArgs& w = shared->window->a;
+  st = pq::launch_window_call(*shared->window, false, stream);
+  if (st != PQ_OK) return st;
+  return pq::launch_merge(w.d, w.n_rows, 2, shared->part_out, PQ_DTYPE_F32, shared->part_lse, shared->out, shared->out_dtype, nullptr, status, stream);
+}
 
 static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
                                 const void* tables_dev, const void* q_dev, int32_t io_dtype, const void* cache_dev,
                                 const int32_t* cache_lens_dev, int32_t batch, int32_t n_q, int32_t capacity, const pq::Paging& pg,
                                 int32_t max_len, float scale, void* out_dev, void* workspace_dev, int32_t* status_dev,
-                                void* stream, float* lse_dev = nullptr, const SharedPrefix* shared = nullptr) {
+                                void* stream, float* lse_dev = nullptr, const pq::SharedPrefix* shared = nullptr) {
   pq::NvtxRange nvtx_range("pq attention");
   const bool causal = shared == nullptr;
   if (!(head_dim == 16 || head_dim == 32 || head_dim == 64 || head_dim == 128)) return PQ_ERR_UNSUPPORTED;
@@ -915,7 +964,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   pq::DecodeArgs a;
   a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.batch = (int)pairs; a.n_q = n_q; a.causal = causal; a.capacity = capacity;
-  a.io_dtype = io_dtype; a.out_dtype = shared ? shared->out_dtype : io_dtype; a.scale = scale; a.S = S_dev; a.tables = reinterpret_cast<const pq::Tables*>(tables_dev);
+  a.io_dtype = io_dtype; a.out_dtype = !shared ? io_dtype : shared->window ? PQ_DTYPE_F32 : shared->out_dtype; a.scale = scale; a.S = S_dev; a.tables = reinterpret_cast<const pq::Tables*>(tables_dev);
   a.q = q_dev; a.cache = reinterpret_cast<const uint8_t*>(cache_dev); a.lens = cache_lens_dev; a.out = out_dev;
   a.status = status_dev;
   a.lse = lse_dev;
@@ -927,6 +976,17 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   pq::SplitCommon c;
   c.d = head_dim; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = io_dtype; c.out_dtype = a.out_dtype; c.scale = scale;
   c.S = S_dev; c.q = q_dev; c.out = out_dev; c.lse = lse_dev; c.status = status_dev;
+  if (shared != nullptr && head_dim != 128) {
+    static pq::DeviceMemo sm_count;
+    const int n_sm = pq::sm_count_of_device(sm_count);
+    if (n_sm == 0) return PQ_ERR_CUDA;
+    const pq::PrefixCut cut = pq::cut_prefix(n_q, n_kv_heads, g, max_len, std::min(n_sm, pq::kFastMaxGridHost));
+    switch (head_dim) {
+      case 16: return pq::launch_prefix<16>(a, *shared, workspace_dev, cut, st);
+      case 32: return pq::launch_prefix<32>(a, *shared, workspace_dev, cut, st);
+      default: return pq::launch_prefix<64>(a, *shared, workspace_dev, cut, st);
+    }
+  }
   if (head_dim == 128) {
     const bool paged = pg.table != nullptr;
     static pq::DeviceMemo sm_count;
@@ -956,9 +1016,14 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     const bool forced = n_q * g <= 32 && pq::take_debug_wait_failure(5), fail_wait = n_q * g <= 32 && pq::take_debug_wait_failure(2);
     pq::AttentionKernel kernel = plan.kernel;
     if ((forced || fail_wait) && kernel == pq::kClusterKernel) kernel = plan.persistent;
+        if (kernel == pq::kTensorKernel && shared != nullptr) {
+      if (getenv("PQ_CTAS") && atoi(getenv("PQ_CTAS")) == 1) return pq::launch_prefix_tc<1>(a, *shared, plan.n_splits, st);
+      return pq::launch_prefix_tc<2>(a, *shared, plan.n_splits, st);
+    }
     if (kernel == pq::kTensorKernel) return pq::launch_prefill_tc(a, batch, n_q, plan.n_splits, st);
     a.debug = fail_wait ? 1u : 0u;
-    if (kernel == pq::kRowsKernel) return pq::launch_rows_attention(a, pq::cut_rows((int64_t)n_q * g), batch, paged, st);
+    if (kernel == pq::kRowsKernel)
+      return then_window(pq::launch_rows_attention(a, pq::cut_rows((int64_t)n_q * g), batch, paged, st), shared, status_dev, st);
     if (kernel == pq::kPersistentKernel) {
       a.epoch = pq::next_epoch();
       static pq::DeviceMemo configured[4];
@@ -966,7 +1031,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
           g <= 4 ? (paged ? pq::decode_attention_fast_kernel<1, true> : pq::decode_attention_fast_kernel<1, false>)
                  : (paged ? pq::decode_attention_fast_kernel<2, true> : pq::decode_attention_fast_kernel<2, false>);
       if (pq::configure_for_device(fast, pq::kFsTotal, configured[(g > 4 ? 2 : 0) + (paged ? 1 : 0)]) == 0) return PQ_ERR_CUDA;
-      return pq::launch_persistent(fast, a, n_sm, pq::kFastThreads, pq::kFsTotal, st);
+      return then_window(pq::launch_persistent(fast, a, n_sm, pq::kFastThreads, pq::kFsTotal, st), shared, status_dev, st);
     }
   }
   switch (head_dim) {
@@ -980,7 +1045,9 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
       if (load.waves * load.tokens < pq::kPairTokens) return pq::dispatch_split_attention(split, pairs, max_len, st);
       return pq::dispatch_split_attention(pq::packed_split<64, true>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
     }
-    default: return pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
+    default:
+      return then_window(pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st),
+                         shared, status_dev, st);
   }
 }
 
@@ -1197,56 +1264,49 @@ int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, 
   return parts > 1 ? parts * rows * (head_dim + 1) * 4 : 16;
 }
 
-static int32_t window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
-                            const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
-                            const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
-                            void* workspace_dev, int32_t* status_dev, void* stream, int out_dtype, bool only_check = false) {
-  pq::NvtxRange nvtx_range("pq_window_attention");
+// The arguments of a window attention, checked; its parts go to workspace_dev.
+static int32_t window_call(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
+                           const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
+                           const pq_paging* paging, int32_t max_len, float scale, void* out_dev, int32_t out_dtype, float* lse_dev,
+                           void* workspace_dev, int32_t* status_dev, pq::WindowCall* call) {
   if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
   if (!q_dev || !pool_dev || !window_lens_dev || !out_dev || !workspace_dev || !status_dev) return PQ_ERR_INVALID_ARG;
   if (batch <= 0 || n_q <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_len <= 0 || n_q_heads % n_kv_heads) return PQ_ERR_INVALID_ARG;
   if ((io_dtype != PQ_DTYPE_F32 && io_dtype != PQ_DTYPE_BF16) || (kv_dtype != PQ_DTYPE_F32 && kv_dtype != PQ_DTYPE_BF16)) return PQ_ERR_UNSUPPORTED;
-  pq::WindowArgs a;
-  int32_t st = pq::window_paging_from(paging, &a.pg);
+  pq::WindowArgs& a = call->a;
+  const int32_t st = pq::window_paging_from(paging, &a.pg);
   if (st != PQ_OK) return st;
   if (((uintptr_t)q_dev | (uintptr_t)pool_dev | (uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
   if (((uintptr_t)window_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
   const int g = n_q_heads / n_kv_heads;
   const pq::WindowRows rows = pq::window_rows(head_dim, kv_dtype, n_q, g);
   if (batch > 65535 || n_kv_heads * rows.blocks > 65535) return PQ_ERR_UNSUPPORTED;
-  if (only_check) return PQ_OK;
-  static pq::DeviceMemo sm_count;
-  const int n_sm = pq::sm_count_of_device(sm_count);
-  if (n_sm == 0) return PQ_ERR_CUDA;
-  const pq::WindowCut cut = pq::window_cut(head_dim, kv_dtype, batch, n_q, n_kv_heads, g, max_len, std::min(n_sm, pq::kFastMaxGridHost));
-  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype;
-  a.row_blocks = (int)rows.blocks; a.n_parts = cut.parts; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
+  call->kv_dtype = kv_dtype; call->rows = rows.rows; call->batch = batch; call->max_len = max_len;
+  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.early = 0;
+  a.row_blocks = (int)rows.blocks; a.n_parts = 1; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
   a.q = q_dev; a.pool = reinterpret_cast<const uint8_t*>(pool_dev); a.lens = window_lens_dev; a.out = out_dev; a.lse = lse_dev;
-  a.part_out = reinterpret_cast<float*>(workspace_dev); a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * head_dim : 0);
+  a.part_out = reinterpret_cast<float*>(workspace_dev); a.part_lse = nullptr;
   a.status = status_dev;
-  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  st = pq::launch_window_attention(a, kv_dtype, rows.rows, batch, cut, s);
-  if (st != PQ_OK || cut.parts == 1) return st;
-  // the window kernel has reported the rows that see nothing
-  return pq::launch_merge(head_dim, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, out_dev, out_dtype, lse_dev, nullptr, s);
+  return PQ_OK;
 }
-
-
 int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const void* q_dev, int32_t io_dtype,
                             const void* pool_dev, int32_t kv_dtype, const int32_t* window_lens_dev, int32_t batch, int32_t n_q,
                             const pq_paging* paging, int32_t max_len, float scale, void* out_dev, float* lse_dev,
                             void* workspace_dev, int32_t* status_dev, void* stream) {
-  return window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, paging, max_len, scale,
-                          out_dev, lse_dev, workspace_dev, status_dev, stream, io_dtype);
+  pq::NvtxRange nvtx_range("pq_window_attention");
+  pq::WindowCall call;
+  const int32_t st = window_call(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, paging, max_len,
+                                 scale, out_dev, io_dtype, lse_dev, workspace_dev, status_dev, &call);
+  return st != PQ_OK ? st : pq::launch_window_call(call, false, reinterpret_cast<cudaStream_t>(stream));
 }
 
 static int32_t prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
-                            const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
-                            const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
-                            int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* out_dev,
-                            float* lse_dev, void* workspace_dev, int32_t* status_dev, void* stream, int out_dtype) {
+                                const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
+                                const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
+                                int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* workspace_dev,
+                                int32_t* status_dev, void* stream, const pq::SharedPrefix& shared) {
   if (cache_batch <= 0 || sequence < 0 || sequence >= cache_batch || !cache_dev || !cache_lens_dev) return PQ_ERR_INVALID_ARG;
-  if (((uintptr_t)cache_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
+  if (((uintptr_t)cache_lens_dev | (uintptr_t)shared.lse | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
   pq::Paging pg;
   const uint8_t* cache = reinterpret_cast<const uint8_t*>(cache_dev);
   if (paging == nullptr) {   // the sequence's own part of the cache, as a cache of one sequence
@@ -1260,18 +1320,26 @@ static int32_t prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     pg.table += (int64_t)sequence * pg.pages_per_seq;
     capacity = pg.page_tokens * pg.pages_per_seq;
   }
-  const SharedPrefix shared = {out_dtype};
+  const bool windowed = shared.window != nullptr;
   return launch_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, cache, cache_lens_dev + sequence, 1, n_queries,
-                          capacity, pg, max_len, scale, out_dev, workspace_dev, status_dev, stream, lse_dev, &shared);
+                          capacity, pg, max_len, scale, windowed ? shared.part_out : shared.out, workspace_dev, status_dev, stream,
+                          windowed ? shared.part_lse : shared.lse, &shared);
 }
-
 int32_t pq_prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads, const float* S_dev,
                             const void* tables_dev, const void* q_dev, int32_t io_dtype, int32_t n_queries,
                             const void* cache_dev, const int32_t* cache_lens_dev, int32_t cache_batch, int32_t sequence,
                             int32_t capacity, const pq_paging* paging, int32_t max_len, float scale, void* out_dev,
                             float* lse_dev, void* workspace_dev, int32_t* status_dev, void* stream) {
+  const pq::SharedPrefix shared = {out_dev, io_dtype, lse_dev, nullptr, nullptr, nullptr};
   return prefix_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, n_queries, cache_dev, cache_lens_dev, cache_batch,
-                          sequence, capacity, paging, max_len, scale, out_dev, lse_dev, workspace_dev, status_dev, stream, io_dtype);
+                          sequence, capacity, paging, max_len, scale, workspace_dev, status_dev, stream, shared);
+}
+
+int64_t pq_prefix_workspace_bytes(int32_t head_dim, int32_t n_queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len) {
+  const int64_t other = pq_workspace_bytes(head_dim, n_queries, n_q_heads, n_kv_heads, max_len);
+  if (other < 0) return other;
+  const pq::PrefixCut cut = pq::cut_prefix(n_queries, n_kv_heads, n_q_heads / n_kv_heads, max_len, pq::kFastMaxGridHost);
+  return std::max(other, pq::prefix_workspace_bytes(head_dim, (int64_t)n_queries * n_q_heads, cut.parts));
 }
 
 // The workspace of pq_shared_attention: two parts of float32 outputs with their log-sum-exps, then what the two attentions need.
@@ -1290,7 +1358,7 @@ static SharedWorkspace shared_workspace(int32_t head_dim, int64_t rows, int64_t 
 int64_t pq_shared_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len,
                                   int32_t max_window) {
   if (batch <= 0 || n_q <= 0 || (int64_t)batch * n_q > 65535) return batch <= 0 || n_q <= 0 ? PQ_ERR_INVALID_ARG : PQ_ERR_UNSUPPORTED;
-  const int64_t prefix = pq_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len);
+  const int64_t prefix = pq_prefix_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len);
   if (prefix < 0) return prefix;
   const int64_t window = pq_window_workspace_bytes(head_dim, batch, n_q, n_q_heads, n_kv_heads, max_window);
   if (window < 0) return window;
@@ -1310,21 +1378,18 @@ int32_t pq_shared_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
   if (!out_dev || !workspace_dev) return PQ_ERR_INVALID_ARG;
   if (((uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
   const int64_t rows = (int64_t)batch * n_q * n_q_heads;
-  const SharedWorkspace at = shared_workspace(head_dim, rows, pq_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len), 0);
+  const SharedWorkspace at = shared_workspace(head_dim, rows, pq_prefix_workspace_bytes(head_dim, batch * n_q, n_q_heads, n_kv_heads, max_len), 0);
   uint8_t* ws = reinterpret_cast<uint8_t*>(workspace_dev);
   float* parts = reinterpret_cast<float*>(ws);
   float* lse = reinterpret_cast<float*>(ws + at.lse);
   // nothing is launched where the window's arguments are refused
-  int32_t st = window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, window_paging,
-                                max_window, scale, parts + rows * head_dim, lse + rows, ws + at.window, status_dev, stream, PQ_DTYPE_F32, true);
+  pq::WindowCall window;
+  const int32_t st = window_call(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, window_paging,
+                                 max_window, scale, parts + rows * head_dim, PQ_DTYPE_F32, lse + rows, ws + at.window, status_dev, &window);
   if (st != PQ_OK) return st;
-  st = prefix_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, batch * n_q, cache_dev, cache_lens_dev,
-                                   cache_batch, sequence, capacity, paging, max_len, scale, parts, lse, ws + at.prefix, status_dev, stream, PQ_DTYPE_F32);
-  if (st != PQ_OK) return st;
-  st = window_attention(head_dim, n_q_heads, n_kv_heads, q_dev, io_dtype, pool_dev, kv_dtype, window_lens_dev, batch, n_q, window_paging,
-                           max_window, scale, parts + rows * head_dim, lse + rows, ws + at.window, status_dev, stream, PQ_DTYPE_F32);
-  if (st != PQ_OK) return st;
-  return pq::launch_merge(head_dim, rows, 2, parts, PQ_DTYPE_F32, lse, out_dev, io_dtype, nullptr, status_dev, reinterpret_cast<cudaStream_t>(stream));
+  const pq::SharedPrefix shared = {out_dev, io_dtype, nullptr, &window, parts, lse};
+  return prefix_attention(head_dim, n_q_heads, n_kv_heads, S_dev, tables_dev, q_dev, io_dtype, batch * n_q, cache_dev, cache_lens_dev, cache_batch,
+                          sequence, capacity, paging, max_len, scale, ws + at.prefix, status_dev, stream, shared);
 }
 
 }  // extern "C"

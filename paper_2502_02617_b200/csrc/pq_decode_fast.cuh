@@ -334,6 +334,7 @@ template <int kThreads>
 __device__ __forceinline__ void build_fast_tables(uint8_t* smem, const Tables* tb) {
   const int tid = threadIdx.x;
   constexpr int kPer = 256 * 16 / kThreads;
+  static_assert(kPer * kThreads == 256 * 16, "every entry has a thread");
   uint2 v[3 * kPer];
 #pragma unroll
   for (int r = 0; r < kPer; ++r) {

@@ -205,7 +205,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prefill_tc_kernel(DecodeArgs a,
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   // the last query of the pair sees the most
   const int q_last = min(n_q, ((int)(blockIdx.x | 1u) + 1) * qb_rows) - 1;
-  const int vis_cta = max(0, len - a.hidden(q_last));
+  const int vis_cta = max(0, len - (n_q - 1 - q_last));
   const int all_blocks = (vis_cta + kTokenBlock - 1) / kTokenBlock;
   const int jb0 = (int)((int64_t)all_blocks * split / n_splits);                       // this pair's blocks are jb0 + jb,
   const int n_blocks = (int)((int64_t)all_blocks * (split + 1) / n_splits) - jb0;      // 0 <= jb < n_blocks
@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(kPtThreads, 1) prefill_tc_kernel(DecodeArgs a,
   if (warp < 4) {
     // ================= row owners: softmax of row `tid` =================
     const int r = tid;
-    const int vis = r < n_rows ? max(0, len - a.hidden(q0 + r / g)) : 0;
+    const int vis = r < n_rows ? max(0, len - (n_q - 1 - (q0 + r / g))) : 0;
     const uint32_t trow = tmem_base + ((uint32_t)(warp * 32) << 16);
     const int vis_min = __reduce_min_sync(0xffffffffu, vis);
     for (int jb = 0; jb < n_blocks; ++jb) {

@@ -182,10 +182,10 @@ __device__ __forceinline__ void store_unrotated(const float* x, const float* s, 
   }
 }
 
-// out = (sum_p exp(lse_p - lse) part_p) S^T of every row, and lse (lse_out, where it is asked for); parts [part][row][128], lse [part][row] (natural log, -inf: nothing seen).
+// out = (sum_p exp(lse_p - lse) part_p) S^T of every row; parts [part][row][128], lse [part][row] (natural log, -inf: nothing seen).
 template <int kTile>
 __global__ void __launch_bounds__(kRotThreads) merge_unrotate_kernel(const float* S, const float* parts, const float* lse, int n_parts,
-                                                                     int64_t n_rows, void* out, int out_dtype, float* lse_out, int32_t* status) {
+                                                                     int64_t n_rows, void* out, int out_dtype, int32_t* status) {
   extern __shared__ __align__(16) float rot_smem[];
   float* s = rot_smem;   // S^T
   float* x = rot_smem + 128 * kRotSStride;
@@ -219,10 +219,8 @@ __global__ void __launch_bounds__(kRotThreads) merge_unrotate_kernel(const float
         }
         const float k = 1.f / wsum;
         acc = make_float4(acc.x * k, acc.y * k, acc.z * k, acc.w * k);
-        if (lse_out != nullptr && lane == 0) lse_out[row] = mx + __logf(wsum);
-      } else if (lane == 0) {   // a query that sees no token: zeros
-        if (lse_out != nullptr) lse_out[row] = -CUDART_INF_F;
-        else set_status(status, PQ_ERR_EMPTY);
+      } else if (lane == 0) {
+        set_status(status, PQ_ERR_EMPTY);   // a query that sees no token: zeros
       }
     }
     *reinterpret_cast<float4*>(x + 4 * i) = acc;
@@ -315,11 +313,11 @@ static int32_t launch_rotate(const float* S, const void* q, int io_dtype, int64_
   });
 }
 static int32_t launch_unrotate(const float* S, const float* parts, const float* lse, int n_parts, int64_t n_rows, void* out, int out_dtype,
-                               float* lse_out, int32_t* status, cudaStream_t stream) {
+                               int32_t* status, cudaStream_t stream) {
   return with_rot_tile(n_rows, [&](auto tile, int n_sm) {
     static DeviceMemo configured;
     return launch_rot_kernel<tile>(merge_unrotate_kernel<tile>, configured, n_rows, n_sm, stream, S, parts, lse, n_parts, n_rows, out, out_dtype,
-                                   lse_out, status);
+                                   status);
   });
 }
 static int32_t launch_merge_rows(const DecodeArgs& a, cudaStream_t stream) {

@@ -171,14 +171,14 @@ __global__ void __launch_bounds__(256) append_window_kernel(const __grid_constan
 
 // A sequence's window grows by its rows, all of them or, where one of them has no place, none.
 __device__ __forceinline__ void advance_window(const AppendArgs& a, int b) {
-  const int base = a.lens[b], count = a.cu_seqlens != nullptr ? a.cu_seqlens[b + 1] - a.cu_seqlens[b] : 1;
+  const int base = __ldcg(a.lens + b), count = a.cu_seqlens != nullptr ? __ldcg(a.cu_seqlens + b + 1) - __ldcg(a.cu_seqlens + b) : 1;
   if (count <= 0 || !append_fits(a, base, count)) return;
   if (a.cu_seqlens != nullptr && a.cu_seqlens[b + 1] > a.total_tokens) {   // rows that do not exist
     set_status(a.status, PQ_ERR_INVALID_ARG);
     return;
   }
   for (int p = base / a.pg.page_tokens; p <= (base + count - 1) / a.pg.page_tokens; ++p)
-    if ((unsigned)a.pg.table[(int64_t)b * a.pg.pages_per_seq + p] >= (unsigned)a.pg.n_pages) return;
+    if ((unsigned)__ldcg(a.pg.table + (int64_t)b * a.pg.pages_per_seq + p) >= (unsigned)a.pg.n_pages) return;
   a.lens[b] = base + count;
 }
 // A thread per sequence, behind a kernel that has every block say (launch_dependents) when it has read the lengths: the windows

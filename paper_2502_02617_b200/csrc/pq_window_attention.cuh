@@ -19,6 +19,8 @@ constexpr int kWinThreads = 128, kWinWarps = kWinThreads / 32, kWinMaxCluster = 
 
 struct WindowArgs {
   int d, n_q_heads, n_kv_heads, n_q, io_dtype, out_dtype, row_blocks, n_parts;
+  int early;            // the kernel ahead in the stream writes nothing that this one reads, and has every block say (launch_dependents)
+                        // when all before it is done: wait for it at the end only, and use the SMs that it leaves idle
   int64_t n_rows;       // batch * n_q * n_q_heads: rows of q, out and of a part
   float scale;
   const void* q;
@@ -76,18 +78,53 @@ __device__ __forceinline__ void win_pairs(uint4 w, uint64_t* x) {
   }
 }
 
-// The last step of a block: the blocks of the cluster merge their outputs y [n_rows][D], relative to (reference, denominator) bl, each
-// block a share of the elements, and store them.
-template <int D, class RowOf, class Seen>
-__device__ __forceinline__ void window_finish(const WindowArgs& a, const float* y, const float2* bl, int n_rows, RowOf row_of, Seen seen) {
+// The outputs o [stream][kRows][D] of a block's streams, relative to ml [stream][kRows] = (reference, denominator), merged into the
+// first one's place.  True if there is a NaN among them; a barrier has passed at the end.
+template <int D, int kThreads, int kStreams, int kRows>
+__device__ __forceinline__ bool merge_streams(float* o, float2* ml, int n_rows) {
+  bool nan = false;
+  float2 merged = make_float2(-CUDART_INF_F, 0.f);   // of row tid
+  const int tid = threadIdx.x;
+  for (int i = tid; i < n_rows * D / 4; i += kThreads) {
+    const int r = i / (D / 4), c = 4 * (i % (D / 4));
+    float M = -CUDART_INF_F;
+#pragma unroll
+    for (int w = 0; w < kStreams; ++w) M = fmaxf(M, ml[w * kRows + r].x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kStreams; ++w) {
+      const float k = win_rescale(ml[w * kRows + r].x, M);
+      const float4 v = *reinterpret_cast<const float4*>(o + (w * kRows + r) * D + c);
+      acc = make_float4(fmaf(v.x, k, acc.x), fmaf(v.y, k, acc.y), fmaf(v.z, k, acc.z), fmaf(v.w, k, acc.w));
+    }
+    nan = nan || acc.x != acc.x || acc.y != acc.y || acc.z != acc.z || acc.w != acc.w;
+    *reinterpret_cast<float4*>(o + r * D + c) = acc;
+  }
+  if (tid < n_rows) {
+#pragma unroll
+    for (int w = 0; w < kStreams; ++w) merged.x = fmaxf(merged.x, ml[w * kRows + tid].x);
+#pragma unroll
+    for (int w = 0; w < kStreams; ++w) merged.y = fmaf(ml[w * kRows + tid].y, win_rescale(ml[w * kRows + tid].x, merged.x), merged.y);
+    nan = nan || merged.y != merged.y;
+  }
+  nan = __syncthreads_or(nan);
+  if (tid < n_rows) ml[tid] = merged;
+  __syncthreads();
+  return nan;
+}
+
+// The last step of a block: the blocks of the cluster merge their outputs y [n_rows][D], relative to (reference, denominator) bl, and
+// each block hands a share of them to store(row, first of four coordinates, the four, log-sum-exp).  Rows that have seen nothing, or
+// only scores of -inf, are zeros and -inf.
+template <int D, int kThreads, class Store>
+__device__ __forceinline__ void cluster_merge(const float* y, const float2* bl, int n_rows, Store store) {
   uint32_t rank, n_blocks;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
   cluster_arrive();
   cluster_wait();
   const uint32_t y_at = (uint32_t)__cvta_generic_to_shared(y), bl_at = (uint32_t)__cvta_generic_to_shared(bl);
-  const int part = blockIdx.x / n_blocks;
-  for (int i = threadIdx.x + kWinThreads * rank; i < n_rows * D / 4; i += kWinThreads * n_blocks) {
+  for (int i = threadIdx.x + kThreads * rank; i < n_rows * D / 4; i += kThreads * n_blocks) {
     const int r = i / (D / 4), c = 4 * (i % (D / 4));
     float2 ml[kWinMaxCluster];
     float4 v[kWinMaxCluster];
@@ -110,10 +147,19 @@ __device__ __forceinline__ void window_finish(const WindowArgs& a, const float* 
       L = fmaf(ml[k].y, w, L);
       acc = make_float4(fmaf(v[k].x, w, acc.x), fmaf(v[k].y, w, acc.y), fmaf(v[k].z, w, acc.z), fmaf(v[k].w, w, acc.w));
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;   // nothing seen, or only scores of -inf: zeros
-    acc = make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    store(r, c, make_float4(acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv), L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f);
+  }
+  cluster_arrive();   // nobody leaves while its shared memory may be read
+  cluster_wait();
+}
+template <int D, class RowOf, class Seen>
+__device__ __forceinline__ void window_finish(const WindowArgs& a, const float* y, const float2* bl, int n_rows, RowOf row_of, Seen seen) {
+  uint32_t n_blocks;
+  asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
+  const int part = blockIdx.x / n_blocks;
+  cluster_merge<D, kWinThreads>(y, bl, n_rows, [&](int r, int c, const float4& acc, float lse) {
     const int64_t row = row_of(r), at = row * D + c;
-    const float lse = L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f;
     if (a.n_parts > 1) {
       *reinterpret_cast<float4*>(a.part_out + part * a.n_rows * D + at) = acc;
       if (c == 0) a.part_lse[part * a.n_rows + row] = lse;
@@ -128,9 +174,14 @@ __device__ __forceinline__ void window_finish(const WindowArgs& a, const float* 
       if (c == 0 && a.lse != nullptr) a.lse[row] = lse;
     }
     if (c == 0 && a.lse == nullptr && part == 0 && seen(r) == 0) set_status(a.status, PQ_ERR_EMPTY);
+  });
+  if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+__device__ __forceinline__ void window_begin(const WindowArgs& a) {
+  if (!a.early) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
   }
-  cluster_arrive();   // nobody leaves while its shared memory may be read
-  cluster_wait();
 }
 
 // Sums of kN values over 2 kOff lanes: every exchange halves the values that a lane holds.
@@ -163,13 +214,12 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, li = lane & (kLanes - 1), group = lane / kLanes;
   const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks, b = blockIdx.z;
   const int r0 = rb * kRows, n_rows = min(kRows, a.n_q * g - r0);   // row r0 + r: query (r0 + r) / g, head hk * g + (r0 + r) % g
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  window_begin(a);
   auto row_of = [&](int r) -> int64_t {   // of q, out and lse
     const int j = (r0 + r) / g;
     return ((int64_t)b * a.n_q + j) * a.n_q_heads + hk * g + (r0 + r - j * g);
   };
-  const int len = min(max(a.lens[b], 0), a.pg.page_tokens * a.pg.pages_per_seq);
+  const int len = min(max(__ldcg(a.lens + b), 0), a.pg.page_tokens * a.pg.pages_per_seq);
   auto seen = [&](int r) { return max(0, len - (a.n_q - 1 - (r0 + r) / g)); };
   const int most = seen(n_rows - 1), least = seen(0);
   // this block's range of the tokens: whole pieces of 16
@@ -207,7 +257,7 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
   int page = t / P, slot = t - page * P, page0 = page;
   auto entries = [&](int first) {
     int e = 0;
-    if ((int64_t)first * P + (int64_t)lane * P < t_end) e = table[first + lane];
+    if ((int64_t)first * P + (int64_t)lane * P < t_end) e = __ldcg(table + first + lane);
     if ((unsigned)e >= (unsigned)a.pg.n_pages) {   // read page 0 instead: no address outside the pool is formed
       set_status(a.status, PQ_ERR_INVALID_ARG);
       e = 0;

@@ -75,14 +75,13 @@ __global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid
   const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks, b = blockIdx.z;
   const int r0 = rb * W::kRows, n_rows = min(W::kRows, a.n_q * g - r0);   // row r0 + r: query (r0 + r) / g, head hk * g + (r0 + r) % g
   const uint32_t sm = (uint32_t)__cvta_generic_to_shared(wm_smem);
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  window_begin(a);
   auto row_of = [&](int r) -> int64_t {   // of q, out and lse
     const int j = (r0 + r) / g;
     return ((int64_t)b * a.n_q + j) * a.n_q_heads + hk * g + (r0 + r - j * g);
   };
   const int P = a.pg.page_tokens;
-  const int len = min(max(a.lens[b], 0), P * a.pg.pages_per_seq);
+  const int len = min(max(__ldcg(a.lens + b), 0), P * a.pg.pages_per_seq);
   auto seen = [&](int r) { return max(0, len - (a.n_q - 1 - (r0 + r) / g)); };
   const int most = seen(n_rows - 1), least = seen(0);
   const int pieces = (most + 15) / 16, n_splits = gridDim.x;
@@ -97,7 +96,7 @@ __global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid
   int t_req = t_begin + stream * kWmTile, page = t_req / P, slot = t_req - page * P, page0 = page;
   auto entries = [&](int first) {   // a register of the warp holds the table's entries from `first` on
     int e = 0;
-    if ((int64_t)first * P + (int64_t)lane * P < t_end) e = table[first + lane];
+    if ((int64_t)first * P + (int64_t)lane * P < t_end) e = __ldcg(table + first + lane);
     if ((unsigned)e >= (unsigned)a.pg.n_pages) {   // read page 0 instead: no address outside the pool is formed
       set_status(a.status, PQ_ERR_INVALID_ARG);
       e = 0;
@@ -275,35 +274,8 @@ __global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid
       for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(o_sm + r * D + 8 * j + 2 * c4) = make_float2(o[j][2 * h], o[j][2 * h + 1]);
   }
   __syncthreads();
-  // ---- the streams of the block, into the first one's place
-  bool nan = false;
-  float2 merged = make_float2(-CUDART_INF_F, 0.f);   // of row tid
-  for (int i = tid; i < n_rows * D / 4; i += kWinThreads) {
-    const int r = i / (D / 4), c = 4 * (i % (D / 4));
-    float M = -CUDART_INF_F;
-#pragma unroll
-    for (int w = 0; w < W::kStreams; ++w) M = fmaxf(M, ml_sm[w * W::kRows + r].x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < W::kStreams; ++w) {
-      const float k = win_rescale(ml_sm[w * W::kRows + r].x, M);
-      const float4 v = *reinterpret_cast<const float4*>(o_sm + (w * W::kRows + r) * D + c);
-      acc = make_float4(fmaf(v.x, k, acc.x), fmaf(v.y, k, acc.y), fmaf(v.z, k, acc.z), fmaf(v.w, k, acc.w));
-    }
-    nan = nan || acc.x != acc.x || acc.y != acc.y || acc.z != acc.z || acc.w != acc.w;
-    *reinterpret_cast<float4*>(o_sm + r * D + c) = acc;
-  }
-  if (tid < n_rows) {
-#pragma unroll
-    for (int w = 0; w < W::kStreams; ++w) merged.x = fmaxf(merged.x, ml_sm[w * W::kRows + tid].x);
-#pragma unroll
-    for (int w = 0; w < W::kStreams; ++w) merged.y = fmaf(ml_sm[w * W::kRows + tid].y, win_rescale(ml_sm[w * W::kRows + tid].x, merged.x), merged.y);
-    nan = nan || merged.y != merged.y;
-  }
-  nan = __syncthreads_or(nan);
-  if (tid < n_rows) ml_sm[tid] = merged;
+  const bool nan = merge_streams<D, kWinThreads, W::kStreams, W::kRows>(o_sm, ml_sm, n_rows);
   if (nan) {
-    __syncthreads();
     window_again<D>(a, b, hk, r0, n_rows, t_begin, t_end, len, o_sm, ml_sm);
   }
   window_finish<D>(a, o_sm, ml_sm, n_rows, row_of, seen);
@@ -359,6 +331,26 @@ static int32_t launch_window_attention(const WindowArgs& a, int kv_dtype, int ro
     case 64: return launch_window_rows<float, 64>(a, rows, batch, cut, stream);
     default: return launch_window_rows<float, 128>(a, rows, batch, cut, stream);
   }
+}
+
+// An attention over a window with its arguments checked, and its launch: its parts, where there are several, lie at a.part_out.
+struct WindowCall {
+  WindowArgs a;
+  int kv_dtype, rows, batch, max_len;
+};
+static int32_t launch_window_call(const WindowCall& w, bool early, cudaStream_t stream) {
+  static DeviceMemo sm_count;
+  const int n_sm = sm_count_of_device(sm_count);
+  if (n_sm == 0) return PQ_ERR_CUDA;
+  WindowArgs a = w.a;
+  const WindowCut cut = window_cut(a.d, w.kv_dtype, w.batch, a.n_q, a.n_kv_heads, a.n_q_heads / a.n_kv_heads, w.max_len, std::min(n_sm, kFastMaxGridHost));
+  a.early = early;
+  a.n_parts = cut.parts;
+  a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * a.d : 0);
+  const int32_t st = launch_window_attention(a, w.kv_dtype, w.rows, w.batch, cut, stream);
+  if (st != PQ_OK || cut.parts == 1) return st;
+  // the window kernel has reported the rows that see nothing
+  return launch_merge(a.d, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, a.out, a.out_dtype, a.lse, nullptr, stream);
 }
 
 }  // namespace pq

@@ -131,6 +131,25 @@ def test_an_empty_prefix(d, R):
     assert bool((out == 0).all()) and cache.status.cpu().tolist()[0] == pq.ERR_EMPTY
 
 
+@pytest.mark.parametrize("d,R", [(128, 4), (128, 90), (64, 20)])
+def test_a_radius_that_is_no_number_spoils_its_own_head_only(d, R):
+    """Stored radii of NaN (an encoder's input that was not finite): the heads that read them are NaN, the others as they were, and
+    so it is with a window behind, empty or not."""
+    n, hq, hkv = 200, 4, 2
+    cache = make_cache([n], hq, hkv, d, capacity=256)
+    q = synthetic.queries(1, R, hq, d, BF16, DEV)
+    w = pq.PagedWindow(R, hq, hkv, d, 16, R, torch.arange(R).view(R, 1), device=DEV)
+    fill_window(w, [0, 5] * (R // 2), 3)
+    good, good_shared = cache.attend_prefix(q).clone(), cache.attend_shared(q, w).clone()
+    half = cache.cache.numel() // hkv                    # the second kv head's part of the cache
+    radii = 64 * (62 * d // 128) - 64 * (d // 8)         # the last plane of a block of 64 tokens
+    cache.cache[half + radii:half + radii + d // 8] = 255   # token 0's radii: NaN
+    out, shared = cache.attend_prefix(q), cache.attend_shared(q, w)
+    torch.cuda.synchronize()
+    for a, b in ((out, good), (shared, good_shared)):
+        assert torch.equal(a[:, :hq // 2], b[:, :hq // 2]) and bool(torch.isnan(a[:, hq // 2:]).all())
+
+
 def test_queries_of_several_positions_are_just_more_queries():
     cache = make_cache([700], 8, 2, 128)
     q = synthetic.queries(5, 12, 8, 128, BF16, DEV)
