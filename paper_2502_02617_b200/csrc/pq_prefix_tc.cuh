@@ -4,7 +4,7 @@
 //
 // A CTA of 24 warps owns 128 (query, head) rows of a kv head and loops over a range of the 64-token blocks; two CTAs share one 256-row
 // MMA (cta_group::2), or a CTA is alone with 128 rows.
-//   * warps 8-22 (decoders) DeQuant the packed blocks into swizzled tiles: keys as fp16 value and residual, values as fp16;
+//   * warp 22 requests the packed blocks, four in flight; warps 8-21 (decoders) DeQuant the packed blocks into swizzled tiles: keys as fp16 value and residual, values as fp16;
 //   * warp 23 issues S = Q'lo K_hi^T + Q'hi K_lo^T + Q'hi K_hi^T into one of four score accumulators and O += P V_hat;
 //   * warps 0-7 (row owners): thread = row and half of a block's tokens.  A row's two threads exchange their maxima through shared memory
 //     and one barrier of the eight warps, take the same lazy reference, and write 16 columns of P each.  80 registers a thread
@@ -17,7 +17,7 @@
 
 namespace pq {
 
-constexpr int kPcOwners = 8, kPcDecoders = 15, kPcMmaWarp = kPcOwners + kPcDecoders, kPcThreads = 32 * (kPcMmaWarp + 1);
+constexpr int kPcOwners = 8, kPcDecoders = 14, kPcFetchWarp = kPcOwners + kPcDecoders, kPcMmaWarp = kPcFetchWarp + 1, kPcThreads = 32 * (kPcMmaWarp + 1);
 // What the CTAs of one MMA hold, two (a pair) or one.  kStages: decoded blocks in flight.  Per CTA: the keys of kKeys tokens -- for each of
 // the two halves of the coordinates the fp16 values of the tokens (128-byte rows) followed by their residuals -- and kCoords
 // coordinates of the values of 64 tokens.  kGroups: warp-sized pieces of a block's decoding in one CTA.
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
       __syncwarp();
       if (lane == 0) pt_arrive_cluster(sb + kPtBarP + 8 * t + to_leader);
     }
-  } else if (warp < kPcMmaWarp) {
+  } else if (warp < kPcFetchWarp) {
     // ================= decoders: packed block -> K_hat hi / lo, V_hat^T =================
     // Pieces of 1 / kGroups of this CTA's part of a block, counted through all blocks, go to the decoder warps in turn.  A piece is 16
     // coordinates of 32 lanes: 8 tokens x the 4 16-blocks of one coordinate half.  First half of the pieces: keys (of tokens 32 rank ..
@@ -246,31 +246,13 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     const int dw = warp - kPcOwners, bi = lane >> 3, t8 = lane & 7;
     const uint32_t rep = (uint32_t)(lane & 15) * 8u, t1 = (sb + kPtT1) | rep, ub = (sb + kPtU) | rep;
     const uint32_t swz = (uint32_t)(t8 * 128 + (((2 * bi) ^ t8) << 4));   // chunk 2 bi of a row's 64-coordinate half, swizzled by the row
-    int fetched = 0, ready = -1;   // blocks requested (decoder warp 0, lane 0); the last block known to have landed and to have a stage
+    int ready = -1;   // the last block known to have landed and to have a stage
     for (int n = dw; n < kGroups * n_blocks; n += kPcDecoders) {
       const int jb = n / kGroups, i = n % kGroups, st = jb % kStages, buf = jb % kPtRawBufs;
       bool ok = true;
-      if (dw == 0) {   // keep up to kPtRawBufs packed blocks in flight; wait only for the one needed now
-        if (lane == 0)
-          while (ok && fetched < n_blocks && fetched < jb + kPtRawBufs) {
-            const int f = fetched % kPtRawBufs;
-            if (fetched >= kPtRawBufs) {
-              const uint32_t ph = (uint32_t)(fetched / kPtRawBufs - 1) & 1u;
-              if (fetched <= jb) ok = tc_mbar_wait(sb + kPtBarRawEmpty + 8 * f, ph, abort_flag);
-              else if (!tc_mbar_test(sb + kPtBarRawEmpty + 8 * f, ph)) break;
-            }
-            if (ok) {
-              tc_mbar_expect_tx(sb + kPtBarRawFull + 8 * f, kPtRawBytes);
-              bulk_load(sb + kPtRaw + f * kPtRawBytes, a.cache + kv_block_pair_offset(L, a.pg, a.n_kv_heads, 0, hk, jb0 + fetched, a.status),
-                        kPtRawBytes, sb + kPtBarRawFull + 8 * f);
-              ++fetched;
-            }
-          }
-        ok = __all_sync(0xffffffffu, ok);
-      }
       if (jb != ready) {
         // stage st is free once the value MMA of block jb - kStages has completed (it also covers that block's score MMAs)
-        if (ok && jb >= kStages) ok = tc_mbar_wait(sb + kPtBarPv + 8 * st, (uint32_t)(jb / kStages - 1) & 1u, abort_flag);
+        if (jb >= kStages) ok = tc_mbar_wait(sb + kPtBarPv + 8 * st, (uint32_t)(jb / kStages - 1) & 1u, abort_flag);
         if (ok) ok = tc_mbar_wait(sb + kPtBarRawFull + 8 * buf, (uint32_t)(jb / kPtRawBufs) & 1u, abort_flag);
         ready = jb;
       }
@@ -324,10 +306,21 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         tc_mbar_arrive(sb + kPtBarRawEmpty + 8 * buf);
       }
     }
-    if (dw == 0 && lane == 0)   // no copy may be in flight when the CTA ends (they are, where a wait gave up)
-      for (int f = max(0, fetched - kPtRawBufs); f < fetched; ++f)
+  } else if (warp == kPcFetchWarp) {
+    // ================= packed blocks on their way: as many as there are buffers, each requested as soon as one is free =================
+    if (lane == 0) {
+      int fetched = 0;
+      for (; fetched < n_blocks; ++fetched) {
+        const int f = fetched % kPtRawBufs;
+        if (fetched >= kPtRawBufs && !tc_mbar_wait(sb + kPtBarRawEmpty + 8 * f, (uint32_t)(fetched / kPtRawBufs - 1) & 1u, abort_flag)) break;
+        tc_mbar_expect_tx(sb + kPtBarRawFull + 8 * f, kPtRawBytes);
+        bulk_load(sb + kPtRaw + f * kPtRawBytes, a.cache + kv_block_pair_offset(L, a.pg, a.n_kv_heads, 0, hk, jb0 + fetched, a.status),
+                  kPtRawBytes, sb + kPtBarRawFull + 8 * f);
+      }
+      for (int f = max(0, fetched - kPtRawBufs); f < fetched; ++f)   // no copy may be in flight when the CTA ends
         for (int i = 0; i < (1 << 20) && !tc_mbar_try(sb + kPtBarRawFull + 8 * (f % kPtRawBufs), (uint32_t)(f / kPtRawBufs) & 1u); ++i)
           __nanosleep(32);
+    }
   } else if (leader) {
     // ================= MMA issuer =================
     // The whole warp goes through the loop and one elected lane issues: the operands of the MMAs are then warp-uniform values.
