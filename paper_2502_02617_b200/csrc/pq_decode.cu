@@ -876,11 +876,30 @@ static int32_t launch_prefill_tc(DecodeArgs a, int batch, int n_q, int n_splits,
   return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.io_dtype, a.status, stream);
 }
 
+// How prefix_tc_kernel is cut: ranges of the blocks; us, the estimate.
+struct PrefixTcPlan {
+  int n_splits;
+  double us;
+};
+// Ranges whose parts the workspace holds: 32 at most, and no more rows of parts than twice 160 CTAs have, or one part.
+__host__ inline int64_t prefix_tc_most_splits(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(kPxMaxParts, 2 * 160 * 128 / rows)); }
+static PrefixTcPlan plan_prefix_tc(int n_queries, int n_kv_heads, int g, int max_len, int n_sm) {
+  const int qb_rows = kPtRows / g;
+  const int64_t q_blocks = ((int64_t)n_queries + qb_rows - 1) / qb_rows, blocks = ((int64_t)max_len + kTokenBlock - 1) / kTokenBlock;
+  const int64_t all_rows = (int64_t)n_queries * n_kv_heads * g, most = std::min(prefix_tc_most_splits(all_rows), blocks);
+  PrefixTcPlan best = {1, 1e30};
+  for (int s = 1; s <= most; ++s) {
+    const int64_t units = (q_blocks + 1) / 2 * n_kv_heads * s, at_once = n_sm / 2;
+    const double waves = (double)((units + at_once - 1) / at_once), work = waves * ((blocks + s - 1) / s);
+    const double us = 18.0 + 0.93 * work + 8.0 * (waves - 1.0) + 0.2e-3 * s * all_rows + 1.5e-3 * all_rows;
+    if (us < best.us) best = {s, us};
+  }
+  return best;
+}
 // The same for queries that all see the whole sequence: prefix_tc_kernel, and what follows it.
-template <int kCtas>
 static int32_t launch_prefix_tc(DecodeArgs a, const SharedPrefix& shared, int n_splits, cudaStream_t stream) {
   static DeviceMemo configured;
-  if (configure_for_device(prefix_tc_kernel<kCtas>, kPcSmTotal, configured) == 0) return PQ_ERR_CUDA;
+  if (configure_for_device(prefix_tc_kernel, kPcSmTotal, configured) == 0) return PQ_ERR_CUDA;
   const int qb_rows = kPtRows / (a.n_q_heads / a.n_kv_heads), q_blocks = (a.n_q + qb_rows - 1) / qb_rows;
   a.n_splits = n_splits;
   const int64_t all_rows = (int64_t)a.batch * a.n_q_heads;   // the workspace: rotated queries, parts, their log-sum-exps
@@ -891,7 +910,7 @@ static int32_t launch_prefix_tc(DecodeArgs a, const SharedPrefix& shared, int n_
   const int32_t st = launch_prefix_rotate<128>(a.S, a.q, a.io_dtype, all_rows, a.scale * 1.4426950408889634f, qrot, stream);
   if (st != PQ_OK) return st;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((q_blocks + kCtas - 1) / kCtas * kCtas, a.n_kv_heads, n_splits);
+  cfg.gridDim = dim3((q_blocks + 1) & ~1, a.n_kv_heads, n_splits);
   cfg.blockDim = dim3(kPcThreads);
   cfg.dynamicSmemBytes = kPcSmTotal;
   cfg.stream = stream;
@@ -899,12 +918,12 @@ static int32_t launch_prefix_tc(DecodeArgs a, const SharedPrefix& shared, int n_
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // set up while the kernel before it finishes (it waits inside)
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCtas;
+  attr[1].val.clusterDim.x = 2;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 2;
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tc_kernel<kCtas>, a);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, prefix_tc_kernel, a);
   if (e != cudaSuccess) {
     note_cuda_error(e);
     cudaGetLastError();
@@ -1016,10 +1035,8 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     const bool forced = n_q * g <= 32 && pq::take_debug_wait_failure(5), fail_wait = n_q * g <= 32 && pq::take_debug_wait_failure(2);
     pq::AttentionKernel kernel = plan.kernel;
     if ((forced || fail_wait) && kernel == pq::kClusterKernel) kernel = plan.persistent;
-        if (kernel == pq::kTensorKernel && shared != nullptr) {
-      if (getenv("PQ_CTAS") && atoi(getenv("PQ_CTAS")) == 1) return pq::launch_prefix_tc<1>(a, *shared, plan.n_splits, st);
-      return pq::launch_prefix_tc<2>(a, *shared, plan.n_splits, st);
-    }
+        if (kernel == pq::kTensorKernel && shared != nullptr)
+      return pq::launch_prefix_tc(a, *shared, pq::plan_prefix_tc(n_q, n_kv_heads, g, max_len, n_sm).n_splits, st);
     if (kernel == pq::kTensorKernel) return pq::launch_prefill_tc(a, batch, n_q, plan.n_splits, st);
     a.debug = fail_wait ? 1u : 0u;
     if (kernel == pq::kRowsKernel)
@@ -1338,8 +1355,10 @@ int32_t pq_prefix_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
 int64_t pq_prefix_workspace_bytes(int32_t head_dim, int32_t n_queries, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len) {
   const int64_t other = pq_workspace_bytes(head_dim, n_queries, n_q_heads, n_kv_heads, max_len);
   if (other < 0) return other;
-  const pq::PrefixCut cut = pq::cut_prefix(n_queries, n_kv_heads, n_q_heads / n_kv_heads, max_len, pq::kFastMaxGridHost);
-  return std::max(other, pq::prefix_workspace_bytes(head_dim, (int64_t)n_queries * n_q_heads, cut.parts));
+  const int64_t rows = (int64_t)n_queries * n_q_heads;
+  const int64_t parts = head_dim == 128 ? pq::prefix_tc_most_splits(rows)
+                                        : pq::cut_prefix(n_queries, n_kv_heads, n_q_heads / n_kv_heads, max_len, pq::kFastMaxGridHost).parts;
+  return std::max(other, pq::prefix_workspace_bytes(head_dim, rows, parts));
 }
 
 // The workspace of pq_shared_attention: two parts of float32 outputs with their log-sum-exps, then what the two attentions need.

@@ -421,57 +421,69 @@ __global__ void __launch_bounds__(kPrThreads) prefix_unrotate_kernel(const float
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   pr_stage<D>(S, pr_smem);   // a constant of the caller
   asm volatile("griddepcontrol.wait;" ::: "memory");   // the parts come from the kernels before this one
+  // a warp merges kMine rows, all of them at a time
+  constexpr int kMine = W::kRows / 8, kAtOnce = kMine < 2 ? kMine : 2;
+  const int col = lane < kRowLanes ? kV * lane : 0;
+#pragma unroll 1
+  for (int i0 = 0; i0 < kMine; i0 += kAtOnce) {
+    float acc[kAtOnce][kV], w_mine[kAtOnce], mx[kAtOnce], other[kAtOnce];
+    int64_t row[kAtOnce];
+    bool seen[kAtOnce];
 #pragma unroll
-  for (int i = 0; i < W::kRows / 8; ++i) {   // a warp per row
-    const int r = warp + 8 * i;
-    const int64_t row = row0 + r;
-    float acc[kV];
-#pragma unroll
-    for (int e = 0; e < kV; ++e) acc[e] = 0.f;
-    if (row < n_rows) {
-      float mine = lane < n_parts ? lse[lane * n_rows + row] : -CUDART_INF_F;
-      const float other = tail != nullptr ? tail_lse[row] : -CUDART_INF_F;
-      float mx = fmaxf(mine, other);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-      float w_tail = 0.f;
-      if (mx > -CUDART_INF_F || __any_sync(0xffffffffu, mine != mine || other != other)) {   // a NaN part makes the row NaN
-        const float w_mine = mine == -CUDART_INF_F ? 0.f : __expf(mine - mx), w_other = other == -CUDART_INF_F ? 0.f : __expf(other - mx);
-        float sum = w_mine;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        sum += w_other;
-        const int col = lane < kRowLanes ? kV * lane : 0;
-#pragma unroll 4
-        for (int p = 0; p < n_parts; ++p) {   // part order
-          const float w = __shfl_sync(0xffffffffu, w_mine, p);
-          const float* src = parts + (p * n_rows + row) * D + col;
-          if constexpr (kV == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(src);
-            acc[0] = fmaf(w, v.x, acc[0]);
-            acc[1] = fmaf(w, v.y, acc[1]);
-            acc[2 % kV] = fmaf(w, v.z, acc[2 % kV]);
-            acc[3 % kV] = fmaf(w, v.w, acc[3 % kV]);
-          } else {
-            const float2 v = *reinterpret_cast<const float2*>(src);
-            acc[0] = fmaf(w, v.x, acc[0]);
-            acc[1] = fmaf(w, v.y, acc[1]);
-          }
-        }
-        const float inv = 1.f / sum;
-#pragma unroll
-        for (int e = 0; e < kV; ++e) acc[e] *= inv;
-        w_tail = w_other == 0.f ? 0.f : w_other * inv;   // not 0 times a NaN
-        if (lane == 0 && lse_out != nullptr) lse_out[row] = mx + __logf(sum);
-      } else if (lane == 0) {   // a query that sees no token: zeros
-        if (lse_out != nullptr) lse_out[row] = -CUDART_INF_F;
-        else set_status(status, PQ_ERR_EMPTY);
-      }
-      if (lane == 0) tail_w[r] = w_tail;
+    for (int i = 0; i < kAtOnce; ++i) {   // rows past the last repeat it
+      row[i] = min(row0 + warp + 8 * (i0 + i), n_rows - 1);
+      w_mine[i] = lane < n_parts ? lse[lane * n_rows + row[i]] : -CUDART_INF_F;
+      other[i] = tail != nullptr ? tail_lse[row[i]] : -CUDART_INF_F;
     }
-    if (lane < kRowLanes)
 #pragma unroll
-      for (int e = 0; e < kV; e += 2) *reinterpret_cast<float2*>(x + r * W::kXStride + kV * lane + e) = make_float2(acc[e], acc[e + 1]);
+    for (int i = 0; i < kAtOnce; ++i) {
+      mx[i] = fmaxf(w_mine[i], other[i]);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], o));
+      seen[i] = mx[i] > -CUDART_INF_F || __any_sync(0xffffffffu, w_mine[i] != w_mine[i] || other[i] != other[i]);   // a NaN part makes the row NaN
+      w_mine[i] = w_mine[i] == -CUDART_INF_F ? 0.f : __expf(w_mine[i] - mx[i]);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) acc[i][e] = 0.f;
+    }
+#pragma unroll 4
+    for (int p = 0; p < n_parts; ++p) {   // part order
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float w = __shfl_sync(0xffffffffu, w_mine[i], p);
+        const float* src = parts + (p * n_rows + row[i]) * D + col;
+        if constexpr (kV == 4) {
+          const float4 v = *reinterpret_cast<const float4*>(src);
+          acc[i][0] = fmaf(w, v.x, acc[i][0]);
+          acc[i][1] = fmaf(w, v.y, acc[i][1]);
+          acc[i][2 % kV] = fmaf(w, v.z, acc[i][2 % kV]);
+          acc[i][3 % kV] = fmaf(w, v.w, acc[i][3 % kV]);
+        } else {
+          const float2 v = *reinterpret_cast<const float2*>(src);
+          acc[i][0] = fmaf(w, v.x, acc[i][0]);
+          acc[i][1] = fmaf(w, v.y, acc[i][1]);
+        }
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      const int r = warp + 8 * (i0 + i);
+      float sum = w_mine[i];
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const float w_other = other[i] == -CUDART_INF_F ? 0.f : __expf(other[i] - mx[i]);
+      sum += w_other;
+      const float inv = seen[i] ? 1.f / sum : 0.f;   // a query that sees no token: zeros (its parts hold zeros)
+      if (lane == 0) {
+        tail_w[r] = w_other == 0.f ? 0.f : w_other * inv;   // not 0 times a NaN
+        if (row0 + r < n_rows) {
+          if (lse_out != nullptr) lse_out[row[i]] = seen[i] ? mx[i] + __logf(sum) : -CUDART_INF_F;
+          else if (!seen[i]) set_status(status, PQ_ERR_EMPTY);
+        }
+      }
+      if (lane < kRowLanes)
+#pragma unroll
+        for (int e = 0; e < kV; e += 2) *reinterpret_cast<float2*>(x + r * W::kXStride + kV * lane + e) = make_float2(acc[i][e] * inv, acc[i][e + 1] * inv);
+    }
   }
   __syncthreads();
   float y[W::kNt][4];
@@ -547,7 +559,7 @@ static PrefixCut cut_prefix(int n_queries, int n_kv_heads, int g, int max_len, i
   return c;
 }
 // The workspace: rotated queries, parts, their log-sum-exps.
-static int64_t prefix_workspace_bytes(int d, int64_t n_rows, int parts) { return n_rows * 4 * d + (int64_t)parts * n_rows * (d + 1) * 4; }
+static int64_t prefix_workspace_bytes(int d, int64_t n_rows, int64_t parts) { return n_rows * 4 * d + parts * n_rows * (d + 1) * 4; }
 
 template <int D, int kTiles>
 static int32_t launch_prefix_mma(const PrefixKernelArgs& a, const PrefixCut& cut, cudaStream_t stream) {

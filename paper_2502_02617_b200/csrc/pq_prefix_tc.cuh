@@ -2,15 +2,18 @@
 // (included by pq_decode.cu): the roles and operands of prefill_tc_kernel, without a causal limit, with twice the row owners and a
 // third more decoders.
 //
-// A CTA of 24 warps owns 128 (query, head) rows of a kv head and loops over a range of the 64-token blocks; two CTAs share one 256-row
-// MMA (cta_group::2), or a CTA is alone with 128 rows.
-//   * warp 22 requests the packed blocks, four in flight; warps 8-21 (decoders) DeQuant the packed blocks into swizzled tiles: keys as fp16 value and residual, values as fp16;
+// A CTA of 24 warps owns 128 (query, head) rows of a kv head, two CTAs share one 256-row MMA (cta_group::2) and loop over a range of the
+// 64-token blocks, each decoding half of a block.
+//   * warp 22 requests the packed blocks, four in flight; with a decoder warp that asks for them between its pieces a block came 7 % later
+//   * warps 8-21 (decoders) DeQuant the packed blocks into swizzled tiles: keys as fp16 value and residual, values as fp16;
 //   * warp 23 issues S = Q'lo K_hi^T + Q'hi K_lo^T + Q'hi K_hi^T into one of four score accumulators and O += P V_hat;
 //   * warps 0-7 (row owners): thread = row and half of a block's tokens.  A row's two threads exchange their maxima through shared memory
 //     and one barrier of the eight warps, take the same lazy reference, and write 16 columns of P each.  80 registers a thread
-//     are enough for half a row, so that 24 warps fit where 16 did: decoding and softmax are bound by the latency of a warp's chain and
-//     by issue.
-// In prefill_tc_kernel four owner warps with a whole row and eleven decoders took ...
+//     are enough for half a row, so that 24 warps fit where 16 do with a whole row.
+// Bound by instruction issue: 0.93 us per block of a pair (prefill_tc_kernel 1.0), 4900 warp instructions per CTA; without the lookups
+// 0.84, without the exponentials 0.82, without both 0.69, and with a third of the score MMAs as well 0.62.  A CTA alone with 128 rows,
+// whole blocks and two stages takes 1.5 us a block and is faster nowhere.  Measured with the rotations, 32/8 heads: 64 queries over 32768
+// tokens 84 us, over 65536 136; 256 over 32768 275.
 #pragma once
 
 #include "pq_tc_common.cuh"
@@ -18,15 +21,6 @@
 namespace pq {
 
 constexpr int kPcOwners = 8, kPcDecoders = 14, kPcFetchWarp = kPcOwners + kPcDecoders, kPcMmaWarp = kPcFetchWarp + 1, kPcThreads = 32 * (kPcMmaWarp + 1);
-// What the CTAs of one MMA hold, two (a pair) or one.  kStages: decoded blocks in flight.  Per CTA: the keys of kKeys tokens -- for each of
-// the two halves of the coordinates the fp16 values of the tokens (128-byte rows) followed by their residuals -- and kCoords
-// coordinates of the values of 64 tokens.  kGroups: warp-sized pieces of a block's decoding in one CTA.
-template <int kCtas>
-struct PcShape {
-  static constexpr int kStages = 2 * kCtas, kKeys = 64 / kCtas, kCoords = 128 / kCtas, kGroups = 32 / kCtas;
-  static constexpr int kKLo = kKeys * 128, kKHalf = 2 * kKLo, kKTile = 2 * kKHalf, kStage = kKTile + 64 * kCoords * 2;
-  static_assert(kStages * kStage == kPtStages * kPtStage && kStages <= kPtStages, "the map of prefill_tc_kernel");
-};
 constexpr uint32_t kPcMax = (kPtMisc + 16 + 15) / 16 * 16;   // floats [2][2][128], behind that map
 constexpr int kPcSmTotal = (int)(kPcMax + 2 * 2 * 128 * 4 - kPtBase);
 static_assert(kPcSmTotal <= 227 * 1024, "shared memory of one CTA");
@@ -44,31 +38,7 @@ __device__ __forceinline__ bool pc_owners_failed(bool fail) {
       : "memory");
   return any != 0;
 }
-// The A operand in tensor memory (lane = row, two 16-bit elements per column, k ascending).  A pair: see tc_mma_ts_pair; alone: 128 rows, all
-// of B.
-template <int kCtas>
-__device__ __forceinline__ void tc_mma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (kCtas == 2) {
-    tc_mma_ts_pair(tmem_d, tmem_a, bdesc, idesc, accumulate);
-  } else {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-  }
-}
-template <int kCtas>
-__device__ __forceinline__ void tc_commit_mma(uint32_t bar) {
-  if constexpr (kCtas == 2) tc_commit_pair(bar);
-  else tc_commit(bar);
-}
-
-template <int kCtas>
 __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) {
-  using W = PcShape<kCtas>;
-  constexpr int kStages = W::kStages, kStage = W::kStage, kKLo = W::kKLo, kKHalf = W::kKHalf, kKTile = W::kKTile, kGroups = W::kGroups;
   extern __shared__ __align__(1024) uint8_t pc_smem_raw[];
   uint8_t* smem = pc_smem_raw - kPtBase;
   const uint32_t sb = tc_smem_u32(pc_smem_raw) - kPtBase;   // the window: rank << 24
@@ -94,18 +64,18 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     set_status(a.status, PQ_ERR_CUDA);
     return;
   }
-  if (tid == 0) {
-    for (int i = 0; i < kStages; ++i) {
-      tc_mbar_init(sb + kPtBarKv + 8 * i, kCtas * kGroups);    // one arrival per decoded piece (of both CTAs)
+  if (warp == kPcFetchWarp && lane == 0) {   // this thread uses some of them before the block has met
+    for (int i = 0; i < kPtStages; ++i) {
+      tc_mbar_init(sb + kPtBarKv + 8 * i, 2 * kPtGroups);    // one arrival per decoded piece (of both CTAs)
       tc_mbar_init(sb + kPtBarPv + 8 * i, 1);                // tcgen05.commit after the value MMA that read the stage
     }
     for (int i = 0; i < kPtRawBufs; ++i) {
       tc_mbar_init(sb + kPtBarRawFull + 8 * i, 1);           // the bytes of a bulk copy
-      tc_mbar_init(sb + kPtBarRawEmpty + 8 * i, kGroups);  // one arrival per decoded piece
+      tc_mbar_init(sb + kPtBarRawEmpty + 8 * i, kPtGroups);  // one arrival per decoded piece
     }
     for (int i = 0; i < kPtScores; ++i) {
       tc_mbar_init(sb + kPtBarS + 8 * i, 1);   // tcgen05.commit
-      tc_mbar_init(sb + kPtBarP + 8 * i, 8 * kCtas);   // one arrival per row-owner warp (of both CTAs)
+      tc_mbar_init(sb + kPtBarP + 8 * i, 2 * kPcOwners);   // one arrival per row-owner warp (of both CTAs)
     }
     tc_mbar_init(sb + kPtBarDrain, 1);
     *abort_flag = 0;
@@ -113,18 +83,25 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
   }
   if (tid < 512) build_fast_tables<512>(smem + kPtTab, a.tables);   // from the caller's tables, which no kernel writes (4096 entries)
   if (warp == kPcMmaWarp) {   // the same warp of both CTAs, the same destination offset
-    if constexpr (kCtas == 2) {
-      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sb + kPtMisc) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    } else {
-      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sb + kPtMisc) : "memory");
-      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(sb + kPtMisc) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   // a programmatic dependent of the kernel before it: its results (lengths, cache, queries) are read only after this wait
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // behind the wait: see WindowArgs::early
   const int len = max(a.lens[0], 0);
+  const int all_blocks = (len + kTokenBlock - 1) / kTokenBlock;
+  const int jb0 = (int)((int64_t)all_blocks * split / n_splits);                       // this pair's blocks are jb0 + jb,
+  const int n_blocks = (int)((int64_t)all_blocks * (split + 1) / n_splits) - jb0;      // 0 <= jb < n_blocks
+  const Layout L = make_layout(128, a.pg.page_tokens);
+  auto request = [&](int j) {   // packed block j of the range
+    const int f = j % kPtRawBufs;
+    tc_mbar_expect_tx(sb + kPtBarRawFull + 8 * f, kPtRawBytes);
+    bulk_load(sb + kPtRaw + f * kPtRawBytes, a.cache + kv_block_pair_offset(L, a.pg, a.n_kv_heads, 0, hk, jb0 + j, a.status), kPtRawBytes,
+              sb + kPtBarRawFull + 8 * f);
+  };
+  if (warp == kPcFetchWarp && lane == 0)   // the first ones are on their way while the queries are brought in
+    for (int j = 0; j < min(kPtRawBufs, n_blocks); ++j) request(j);
   // ---- Q' (fp16 value | residual, rotate_rows_kernel) of this CTA's rows: staged in shared memory with coalesced copies, then
   // written to tensor memory by the row owners (lane = row, two k values per column).  Rows that do not exist repeat the
   // last one (they are not stored).
@@ -159,12 +136,8 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
   __syncthreads();   // Q' is in tensor memory; the staging is dead: the stages may be written
   pt_cluster_sync();   // both CTAs' barriers are initialised and both halves of Q' are in place
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  const int all_blocks = (len + kTokenBlock - 1) / kTokenBlock;
-  const int jb0 = (int)((int64_t)all_blocks * split / n_splits);                       // this pair's blocks are jb0 + jb,
-  const int n_blocks = (int)((int64_t)all_blocks * (split + 1) / n_splits) - jb0;      // 0 <= jb < n_blocks
   // where this CTA's warps announce themselves: the barriers of the even CTA
   const uint32_t to_leader = pt_mapa(sb + kPtBase, 0u) - (sb + kPtBase);   // + a local shared address: that place in the even CTA (cluster window)
-  const Layout L = make_layout(128, a.pg.page_tokens);
 
   float l_run = 0.f, m_run = -CUDART_INF_F;   // row owners: this thread's share of the row's denominator, and the row's reference
   float* row_max = reinterpret_cast<float*>(smem + kPcMax);   // [block parity][half][row]
@@ -202,7 +175,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         const float corr = m_run == -CUDART_INF_F ? 1.f : fast_exp2(m_run - m_new);   // nothing accumulated yet: nothing to scale
         if (jb > 0) {
           // the value MMAs up to block jb - 1 must have completed before the accumulator is touched
-          fail = !__all_sync(0xffffffffu, tc_mbar_wait(sb + kPtBarPv + 8 * ((jb - 1) % kStages), (uint32_t)((jb - 1) / kStages) & 1u, abort_flag));
+          fail = !__all_sync(0xffffffffu, tc_mbar_wait(sb + kPtBarPv + 8 * ((jb - 1) % kPtStages), (uint32_t)((jb - 1) / kPtStages) & 1u, abort_flag));
           if (fail) continue;   // to the next block's barrier
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
@@ -240,27 +213,25 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     }
   } else if (warp < kPcFetchWarp) {
     // ================= decoders: packed block -> K_hat hi / lo, V_hat^T =================
-    // Pieces of 1 / kGroups of this CTA's part of a block, counted through all blocks, go to the decoder warps in turn.  A piece is 16
-    // coordinates of 32 lanes: 8 tokens x the 4 16-blocks of one coordinate half.  First half of the pieces: keys (of tokens 32 rank ..
-    // + 31 in a pair); second half: values (of coordinates 64 rank .. + 63 in a pair).
+    // Pieces of 1 / kPtGroups of this CTA's half of a block, counted through all blocks, go to the decoder warps in turn.  A piece is 16
+    // coordinates of 32 lanes: 8 tokens x the 4 16-blocks of one coordinate half.  Pieces 0-7: the keys of tokens 32 rank .. + 31;
+    // pieces 8-15: the values of coordinates 64 rank .. + 63 of all 64 tokens.
     const int dw = warp - kPcOwners, bi = lane >> 3, t8 = lane & 7;
     const uint32_t rep = (uint32_t)(lane & 15) * 8u, t1 = (sb + kPtT1) | rep, ub = (sb + kPtU) | rep;
     const uint32_t swz = (uint32_t)(t8 * 128 + (((2 * bi) ^ t8) << 4));   // chunk 2 bi of a row's 64-coordinate half, swizzled by the row
     int ready = -1;   // the last block known to have landed and to have a stage
-    for (int n = dw; n < kGroups * n_blocks; n += kPcDecoders) {
-      const int jb = n / kGroups, i = n % kGroups, st = jb % kStages, buf = jb % kPtRawBufs;
+    for (int n = dw; n < kPtGroups * n_blocks; n += kPcDecoders) {
+      const int jb = n / kPtGroups, i = n % kPtGroups, st = jb % kPtStages, buf = jb % kPtRawBufs;
       bool ok = true;
       if (jb != ready) {
-        // stage st is free once the value MMA of block jb - kStages has completed (it also covers that block's score MMAs)
-        if (jb >= kStages) ok = tc_mbar_wait(sb + kPtBarPv + 8 * st, (uint32_t)(jb / kStages - 1) & 1u, abort_flag);
+        // stage st is free once the value MMA of block jb - kPtStages has completed (it also covers that block's score MMAs)
+        if (jb >= kPtStages) ok = tc_mbar_wait(sb + kPtBarPv + 8 * st, (uint32_t)(jb / kPtStages - 1) & 1u, abort_flag);
         if (ok) ok = tc_mbar_wait(sb + kPtBarRawFull + 8 * buf, (uint32_t)(jb / kPtRawBufs) & 1u, abort_flag);
         ready = jb;
       }
       if (!__all_sync(0xffffffffu, ok)) break;
-      const bool is_v = i >= kGroups / 2;
-      // alone: both halves of the coordinates, all tokens
-      const int side = kCtas == 1 ? (i >> 3) & 1 : is_v ? (int)crank : (i >> 2) & 1;
-      const int tok = 8 * (kCtas == 1 || is_v ? i & 7 : (i & 3) + 4 * (int)crank) + t8, blk = 4 * side + bi;
+      const bool is_v = i >= kPtGroups / 2;
+      const int side = is_v ? (int)crank : (i >> 2) & 1, tok = 8 * (is_v ? i & 7 : (i & 3) + 4 * (int)crank) + t8, blk = 4 * side + bi;
       const bool live = (jb0 + jb) * kTokenBlock + tok < len;   // stale bytes past the sequence end must not reach the MMAs
       const uint32_t raw = sb + kPtRaw + buf * kPtRawBytes + (is_v ? kBlockBytes128 : 0);
       const uint32_t l1 = lds32(raw + tok * 32 + blk * 4);
@@ -277,11 +248,11 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         sub_block_hilo<1>(ref, t1, h[2], h[3], l[2], l[3]);
         sub_block_hilo<2>(ref, t1, h[4], h[5], l[4], l[5]);
         sub_block_hilo<3>(ref, t1, h[6], h[7], l[6], l[7]);
-        const uint32_t dst = sb + kPtKv + st * kStage + side * kKHalf + (i & (kGroups / 4 - 1)) * 1024 + swz;
+        const uint32_t dst = sb + kPtKv + st * kPtStage + side * kPtKHalf + (i & 3) * 1024 + swz;
         pt_sts128(dst, as_u32(h[0]), as_u32(h[1]), as_u32(h[2]), as_u32(h[3]));
         pt_sts128(dst ^ 16u, as_u32(h[4]), as_u32(h[5]), as_u32(h[6]), as_u32(h[7]));
-        pt_sts128(dst + kKLo, as_u32(l[0]), as_u32(l[1]), as_u32(l[2]), as_u32(l[3]));
-        pt_sts128((dst + kKLo) ^ 16u, as_u32(l[4]), as_u32(l[5]), as_u32(l[6]), as_u32(l[7]));
+        pt_sts128(dst + kPtKLo, as_u32(l[0]), as_u32(l[1]), as_u32(l[2]), as_u32(l[3]));
+        pt_sts128((dst + kPtKLo) ^ 16u, as_u32(l[4]), as_u32(l[5]), as_u32(l[6]), as_u32(l[7]));
       } else {
         __half2 x[4], y[4];
         sub_block_h2<0>(ref, t1, x[0], y[0]);
@@ -295,7 +266,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
           w[2 * s] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x5410);
           w[2 * s + 1] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x7632);
         }
-        const uint32_t dst = sb + kPtKv + st * kStage + kKTile + (kCtas == 1 ? side * 8192 : 0) + (i & 7) * 1024 + swz;
+        const uint32_t dst = sb + kPtKv + st * kPtStage + kPtKTile + (i & 7) * 1024 + swz;
         pt_sts128(dst, w[0], w[1], w[2], w[3]);
         pt_sts128(dst ^ 16u, w[4], w[5], w[6], w[7]);
       }
@@ -309,13 +280,10 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
   } else if (warp == kPcFetchWarp) {
     // ================= packed blocks on their way: as many as there are buffers, each requested as soon as one is free =================
     if (lane == 0) {
-      int fetched = 0;
+      int fetched = min(kPtRawBufs, n_blocks);
       for (; fetched < n_blocks; ++fetched) {
-        const int f = fetched % kPtRawBufs;
-        if (fetched >= kPtRawBufs && !tc_mbar_wait(sb + kPtBarRawEmpty + 8 * f, (uint32_t)(fetched / kPtRawBufs - 1) & 1u, abort_flag)) break;
-        tc_mbar_expect_tx(sb + kPtBarRawFull + 8 * f, kPtRawBytes);
-        bulk_load(sb + kPtRaw + f * kPtRawBytes, a.cache + kv_block_pair_offset(L, a.pg, a.n_kv_heads, 0, hk, jb0 + fetched, a.status),
-                  kPtRawBytes, sb + kPtBarRawFull + 8 * f);
+        if (!tc_mbar_wait(sb + kPtBarRawEmpty + 8 * (fetched % kPtRawBufs), (uint32_t)(fetched / kPtRawBufs - 1) & 1u, abort_flag)) break;
+        request(fetched);
       }
       for (int f = max(0, fetched - kPtRawBufs); f < fetched; ++f)   // no copy may be in flight when the CTA ends
         for (int i = 0; i < (1 << 20) && !tc_mbar_try(sb + kPtBarRawFull + 8 * (f % kPtRawBufs), (uint32_t)(f / kPtRawBufs) & 1u); ++i)
@@ -326,8 +294,8 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     // The whole warp goes through the loop and one elected lane issues: the operands of the MMAs are then warp-uniform values.
     // From a single thread's registers every MMA took 60 cycles to issue, more than it runs.
     // the value operand is MN-major: [token][coordinate] rows of 64 coordinates, one half per CTA
-    constexpr uint32_t idesc_qk = tc_idesc(false, 128 * kCtas, 64);   // 64 tokens
-    constexpr uint32_t idesc_pv = tc_idesc(false, 128 * kCtas, 128) | (1u << 16);
+    constexpr uint32_t idesc_qk = tc_idesc(false, 256, 64);   // 64 tokens
+    constexpr uint32_t idesc_pv = tc_idesc(false, 256, 128) | (1u << 16);
     uint64_t vdesc_hi = (uint64_t)(1024 >> 4) << 32;   // stride between groups of 8 tokens
     vdesc_hi |= (uint64_t)1 << 46;
     vdesc_hi |= (uint64_t)2 << 61;
@@ -336,31 +304,31 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     const int blocks = __shfl_sync(0xffffffffu, n_blocks, 0);
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem_base, 0);
     auto issue_pv = [&](int jb) {   // O (+)= P_jb V_hat_jb
-      const int t = jb % kPtScores, st = jb % kStages;
+      const int t = jb % kPtScores, st = jb % kPtStages;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t v_lo = ((kPtKv + st * kStage + kKTile) >> 4) | vdesc_lbo;
+      const uint32_t v_lo = ((kPtKv + st * kPtStage + kPtKTile) >> 4) | vdesc_lbo;
       if (tc_elect()) {
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)   // 16 tokens = 8 columns of P = 16 rows of 128 bytes of V_hat per step
-          tc_mma_ts<kCtas>(tm + kPtTmO, tm + kPtTmS + 64 * t + 8 * kk, vdesc_hi | (v_lo + 128 * kk), idesc_pv, (jb > 0 || kk > 0) ? 1u : 0u);
-        tc_commit_mma<kCtas>(sb + kPtBarPv + 8 * st);   // the stage is free, the output accumulator holds block jb
+          tc_mma_ts_pair(tm + kPtTmO, tm + kPtTmS + 64 * t + 8 * kk, vdesc_hi | (v_lo + 128 * kk), idesc_pv, (jb > 0 || kk > 0) ? 1u : 0u);
+        tc_commit_pair(sb + kPtBarPv + 8 * st);   // the stage is free, the output accumulator holds block jb
       }
     };
     auto issue_qk = [&](int jb) {   // S_jb = Q'lo K_hi^T + Q'hi K_lo^T + Q'hi K_hi^T, the small terms first
-      const int t = jb % kPtScores, st = jb % kStages;
+      const int t = jb % kPtScores, st = jb % kPtStages;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t kb = (uint32_t)tc_smem_desc(kPtKv + st * kStage);
+      const uint32_t kb = (uint32_t)tc_smem_desc(kPtKv + st * kPtStage);
       if (tc_elect()) {
 #pragma unroll
         for (int term = 0; term < 3; ++term) {
           const uint32_t qa = tm + (term == 0 ? kPtTmQlo : kPtTmQhi);
 #pragma unroll
           for (int ks = 0; ks < 8; ++ks) {   // 16 k values = 8 columns of Q' per step; step ks: half ks >> 2, 32 bytes per step
-            const uint32_t koff = (uint32_t)((ks >> 2) * kKHalf + (ks & 3) * 32 + (term == 1 ? kKLo : 0)) >> 4;
-            tc_mma_ts<kCtas>(tm + kPtTmS + 64 * t, qa + 8 * ks, desc_hi | (kb + koff), idesc_qk, (term | ks) ? 1u : 0u);
+            const uint32_t koff = (uint32_t)((ks >> 2) * kPtKHalf + (ks & 3) * 32 + (term == 1 ? kPtKLo : 0)) >> 4;
+            tc_mma_ts_pair(tm + kPtTmS + 64 * t, qa + 8 * ks, desc_hi | (kb + koff), idesc_qk, (term | ks) ? 1u : 0u);
           }
         }
-        tc_commit_mma<kCtas>(sb + kPtBarS + 8 * t);
+        tc_commit_pair(sb + kPtBarS + 8 * t);
       }
     };
     // Value MMAs go first when their P is ready (they free a stage for the decoders); the score MMAs run up to kPtScores - 1
@@ -373,7 +341,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         issue_pv(pv++);
         idle = 0;
       } else if (qk < blocks && qk < pv + kPtScores &&
-                 __all_sync(0xffffffffu, tc_mbar_test(sb + kPtBarKv + 8 * (qk % kStages), (uint32_t)(qk / kStages) & 1u))) {
+                 __all_sync(0xffffffffu, tc_mbar_test(sb + kPtBarKv + 8 * (qk % kPtStages), (uint32_t)(qk / kPtStages) & 1u))) {
         issue_qk(qk++);
         idle = 0;
       } else if (++idle > 32) {   // bounded like every wait
@@ -386,7 +354,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     }
     if (blocks > 0) {
       // every MMA issued above has completed when this commit arrives (nothing was issued without blocks: no commit)
-      if (tc_elect()) tc_commit_mma<kCtas>(sb + kPtBarDrain);
+      if (tc_elect()) tc_commit_pair(sb + kPtBarDrain);
       bool drained = false;
       for (int i = 0; i < (1 << 20) && !drained; ++i) {
         drained = tc_mbar_try(sb + kPtBarDrain, 0);
@@ -395,7 +363,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
       if (!drained) *abort_flag = 1;
     }
     __syncwarp();
-    if (kCtas == 2 && lane == 0 && *abort_flag)   // tell the other CTA, whose warps wait for commits that will not come
+    if (lane == 0 && *abort_flag)   // tell the other CTA, whose warps wait for commits that will not come
       asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(kPtMisc + 4 - kPtBase + pt_mapa(sb + kPtBase, 1u)), "r"(1u) : "memory");
   } else if (lane == 0) {
     // the odd CTA of a pair: its operands are read until the even CTA's last commit arrives here too
@@ -444,8 +412,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
   pt_cluster_sync();
   if (warp == kPcMmaWarp) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    if constexpr (kCtas == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
-    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem_base) : "memory");
   }
   if (tid == 0 && aborted) set_status(a.status, PQ_ERR_TIMEOUT);
   for (int i = tid; i < n_rows * 32; i += kPcThreads)
