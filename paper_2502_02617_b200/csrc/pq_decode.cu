@@ -876,23 +876,23 @@ static int32_t launch_prefill_tc(DecodeArgs a, int batch, int n_q, int n_splits,
   return launch_unrotate(a.S, a.part_out, a.part_lse, n_splits, all_rows, a.out, a.io_dtype, a.status, stream);
 }
 
-// How prefix_tc_kernel is cut: ranges of the blocks; us, the estimate.
-struct PrefixTcPlan {
-  int n_splits;
-  double us;
-};
-// Ranges whose parts the workspace holds: 32 at most, and no more rows of parts than twice 160 CTAs have, or one part.
+// Ranges of the blocks that prefix_tc_kernel is cut into.  The workspace holds their parts: 32 at most, and no more rows of parts than twice
+// 160 CTAs have, or one part.  The estimate: waves of pairs at 0.93 us a block, 8 us for a further wave, and a row's share of writing and
+// merging the parts (64 queries over 32768 tokens, 32/8 heads, 4, 9 and 18 ranges: 151, 86 and 100 us; over 2000: 31, 30 and 45).
 __host__ inline int64_t prefix_tc_most_splits(int64_t rows) { return std::max<int64_t>(1, std::min<int64_t>(kPxMaxParts, 2 * 160 * 128 / rows)); }
-static PrefixTcPlan plan_prefix_tc(int n_queries, int n_kv_heads, int g, int max_len, int n_sm) {
+static int prefix_tc_splits(int n_queries, int n_kv_heads, int g, int max_len, int n_sm) {
   const int qb_rows = kPtRows / g;
   const int64_t q_blocks = ((int64_t)n_queries + qb_rows - 1) / qb_rows, blocks = ((int64_t)max_len + kTokenBlock - 1) / kTokenBlock;
-  const int64_t all_rows = (int64_t)n_queries * n_kv_heads * g, most = std::min(prefix_tc_most_splits(all_rows), blocks);
-  PrefixTcPlan best = {1, 1e30};
+  const int64_t all_rows = (int64_t)n_queries * n_kv_heads * g, most = std::min(prefix_tc_most_splits(all_rows), blocks), at_once = n_sm / 2;
+  int best = 1;
+  double least = 1e30;
   for (int s = 1; s <= most; ++s) {
-    const int64_t units = (q_blocks + 1) / 2 * n_kv_heads * s, at_once = n_sm / 2;
-    const double waves = (double)((units + at_once - 1) / at_once), work = waves * ((blocks + s - 1) / s);
-    const double us = 18.0 + 0.93 * work + 8.0 * (waves - 1.0) + 0.2e-3 * s * all_rows + 1.5e-3 * all_rows;
-    if (us < best.us) best = {s, us};
+    const int64_t units = (q_blocks + 1) / 2 * n_kv_heads * s;
+    const double waves = (double)((units + at_once - 1) / at_once), us = waves * (0.93 * ((blocks + s - 1) / s) + 8.0) + 0.2e-3 * s * all_rows;
+    if (us < least) {
+      least = us;
+      best = s;
+    }
   }
   return best;
 }
@@ -1036,7 +1036,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     pq::AttentionKernel kernel = plan.kernel;
     if ((forced || fail_wait) && kernel == pq::kClusterKernel) kernel = plan.persistent;
         if (kernel == pq::kTensorKernel && shared != nullptr)
-      return pq::launch_prefix_tc(a, *shared, pq::plan_prefix_tc(n_q, n_kv_heads, g, max_len, n_sm).n_splits, st);
+      return pq::launch_prefix_tc(a, *shared, pq::prefix_tc_splits(n_q, n_kv_heads, g, max_len, n_sm), st);
     if (kernel == pq::kTensorKernel) return pq::launch_prefill_tc(a, batch, n_q, plan.n_splits, st);
     a.debug = fail_wait ? 1u : 0u;
     if (kernel == pq::kRowsKernel)
