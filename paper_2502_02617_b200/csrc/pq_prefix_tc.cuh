@@ -20,6 +20,7 @@
 
 namespace pq {
 
+constexpr int kPcGroups = 8;   // warp-sized pieces of a block's decoding in a CTA
 constexpr int kPcOwners = 8, kPcDecoders = 14, kPcFetchWarp = kPcOwners + kPcDecoders, kPcMmaWarp = kPcFetchWarp + 1, kPcThreads = 32 * (kPcMmaWarp + 1);
 constexpr uint32_t kPcMax = (kPtMisc + 16 + 15) / 16 * 16;   // floats [2][2][128], behind that map
 constexpr int kPcSmTotal = (int)(kPcMax + 2 * 2 * 128 * 4 - kPtBase);
@@ -66,12 +67,12 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
   }
   if (warp == kPcFetchWarp && lane == 0) {   // this thread uses some of them before the block has met
     for (int i = 0; i < kPtStages; ++i) {
-      tc_mbar_init(sb + kPtBarKv + 8 * i, 2 * kPtGroups);    // one arrival per decoded piece (of both CTAs)
+      tc_mbar_init(sb + kPtBarKv + 8 * i, 2 * kPcGroups);    // one arrival per decoded piece (of both CTAs)
       tc_mbar_init(sb + kPtBarPv + 8 * i, 1);                // tcgen05.commit after the value MMA that read the stage
     }
     for (int i = 0; i < kPtRawBufs; ++i) {
       tc_mbar_init(sb + kPtBarRawFull + 8 * i, 1);           // the bytes of a bulk copy
-      tc_mbar_init(sb + kPtBarRawEmpty + 8 * i, kPtGroups);  // one arrival per decoded piece
+      tc_mbar_init(sb + kPtBarRawEmpty + 8 * i, kPcGroups);  // one arrival per decoded piece
     }
     for (int i = 0; i < kPtScores; ++i) {
       tc_mbar_init(sb + kPtBarS + 8 * i, 1);   // tcgen05.commit
@@ -200,9 +201,11 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
       for (int e = 0; e < 16; ++e) {
         float x0, x1;
         pt_add2(s[2 * e], s[2 * e + 1], -m_use, -m_use, x0, x1);
-        const __half2 p2 = __floats2half2_rn(fast_exp2(x0), fast_exp2(x1));
-        pw[e] = as_u32(p2);
-        pt_add_halves(sum4[e & 3], pw[e]);   // the denominator of what the MMA will see
+        x0 = fast_exp2(x0);
+        x1 = fast_exp2(x1);
+        pw[e] = as_u32(__floats2half2_rn(x0, x1));
+        // the denominator before the rounding to fp16, which is as often up as down: its sum is off by 2^-12 of a weight's share
+        pt_add2(sum4[2 * (e & 1)], sum4[2 * (e & 1) + 1], x0, x1, sum4[2 * (e & 1)], sum4[2 * (e & 1) + 1]);
       }
       tc_st16u_nowait(trow + kPtTmS + 64 * t + 16 * half, pw);
       l_run += (sum4[0] + sum4[1]) + (sum4[2] + sum4[3]);
@@ -213,15 +216,15 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
     }
   } else if (warp < kPcFetchWarp) {
     // ================= decoders: packed block -> K_hat hi / lo, V_hat^T =================
-    // Pieces of 1 / kPtGroups of this CTA's half of a block, counted through all blocks, go to the decoder warps in turn.  A piece is 16
-    // coordinates of 32 lanes: 8 tokens x the 4 16-blocks of one coordinate half.  Pieces 0-7: the keys of tokens 32 rank .. + 31;
-    // pieces 8-15: the values of coordinates 64 rank .. + 63 of all 64 tokens.
+    // Pieces of 1 / kPcGroups of this CTA's half of a block, counted through all blocks, go to the decoder warps in turn.  A piece is twice
+    // 16 coordinates of 32 lanes = 8 tokens x 4 16-blocks: pieces 0-3 both halves of the coordinates of the keys of tokens 32 rank ..
+    // + 31, pieces 4-7 the values of coordinates 64 rank .. + 63 of all 64 tokens.  (Pieces of one 16 coordinates: ... us.)
     const int dw = warp - kPcOwners, bi = lane >> 3, t8 = lane & 7;
     const uint32_t rep = (uint32_t)(lane & 15) * 8u, t1 = (sb + kPtT1) | rep, ub = (sb + kPtU) | rep;
     const uint32_t swz = (uint32_t)(t8 * 128 + (((2 * bi) ^ t8) << 4));   // chunk 2 bi of a row's 64-coordinate half, swizzled by the row
     int ready = -1;   // the last block known to have landed and to have a stage
-    for (int n = dw; n < kPtGroups * n_blocks; n += kPcDecoders) {
-      const int jb = n / kPtGroups, i = n % kPtGroups, st = jb % kPtStages, buf = jb % kPtRawBufs;
+    for (int n = dw; n < kPcGroups * n_blocks; n += kPcDecoders) {
+      const int jb = n / kPcGroups, i = n % kPcGroups, st = jb % kPtStages, buf = jb % kPtRawBufs;
       bool ok = true;
       if (jb != ready) {
         // stage st is free once the value MMA of block jb - kPtStages has completed (it also covers that block's score MMAs)
@@ -230,45 +233,62 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         ready = jb;
       }
       if (!__all_sync(0xffffffffu, ok)) break;
-      const bool is_v = i >= kPtGroups / 2;
-      const int side = is_v ? (int)crank : (i >> 2) & 1, tok = 8 * (is_v ? i & 7 : (i & 3) + 4 * (int)crank) + t8, blk = 4 * side + bi;
-      const bool live = (jb0 + jb) * kTokenBlock + tok < len;   // stale bytes past the sequence end must not reach the MMAs
+      const bool is_v = i >= kPcGroups / 2;
       const uint32_t raw = sb + kPtRaw + buf * kPtRawBytes + (is_v ? kBlockBytes128 : 0);
-      const uint32_t l1 = lds32(raw + tok * 32 + blk * 4);
-      const uint32_t c2 = lds8(raw + kO2 + tok * 8 + blk);
-      const uint32_t c3 = lds8(raw + kO3 + tok * 4 + (blk >> 1)) >> (4 * (blk & 1));
-      const uint32_t c4 = (lds16(raw + kO4 + tok * 2) >> (2 * blk)) & 3u;
-      const uint32_t rbits = lds16(raw + kORad + tok * 16 + blk * 2);
-      const uint32_t rr = live ? rbits | (rbits << 16) : 0u;
-      const BlockRef ref = make_block_ref(l1, c2, c3, c4, as_h2(rr), ub);
       if (!is_v) {
-        // the key as an unevaluated sum hi + lo, coordinates in the order of the lookups: (4s, 4s+2), (4s+1, 4s+3)
-        __half2 h[8], l[8];
-        sub_block_hilo<0>(ref, t1, h[0], h[1], l[0], l[1]);
-        sub_block_hilo<1>(ref, t1, h[2], h[3], l[2], l[3]);
-        sub_block_hilo<2>(ref, t1, h[4], h[5], l[4], l[5]);
-        sub_block_hilo<3>(ref, t1, h[6], h[7], l[6], l[7]);
-        const uint32_t dst = sb + kPtKv + st * kPtStage + side * kPtKHalf + (i & 3) * 1024 + swz;
-        pt_sts128(dst, as_u32(h[0]), as_u32(h[1]), as_u32(h[2]), as_u32(h[3]));
-        pt_sts128(dst ^ 16u, as_u32(h[4]), as_u32(h[5]), as_u32(h[6]), as_u32(h[7]));
-        pt_sts128(dst + kPtKLo, as_u32(l[0]), as_u32(l[1]), as_u32(l[2]), as_u32(l[3]));
-        pt_sts128((dst + kPtKLo) ^ 16u, as_u32(l[4]), as_u32(l[5]), as_u32(l[6]), as_u32(l[7]));
-      } else {
-        __half2 x[4], y[4];
-        sub_block_h2<0>(ref, t1, x[0], y[0]);
-        sub_block_h2<1>(ref, t1, x[1], y[1]);
-        sub_block_h2<2>(ref, t1, x[2], y[2]);
-        sub_block_h2<3>(ref, t1, x[3], y[3]);
-        // coordinates in natural order: (4s, 4s+1) = (x.lo, y.lo), (4s+2, 4s+3) = (x.hi, y.hi)
-        uint32_t w[8];
+        const int tok = 8 * ((i & 3) + 4 * (int)crank) + t8;
+        const bool live = (jb0 + jb) * kTokenBlock + tok < len;   // stale bytes past the sequence end must not reach the MMAs
+        const uint32_t c4w = lds16(raw + kO4 + tok * 2) >> (2 * bi);
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-          w[2 * s] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x5410);
-          w[2 * s + 1] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x7632);
+        for (int side = 0; side < 2; ++side) {
+          const int blk = 4 * side + bi;
+          const uint32_t l1 = lds32(raw + tok * 32 + blk * 4);
+          const uint32_t c2 = lds8(raw + kO2 + tok * 8 + blk);
+          const uint32_t c3 = lds8(raw + kO3 + tok * 4 + (blk >> 1)) >> (4 * (bi & 1));
+          const uint32_t rbits = lds16(raw + kORad + tok * 16 + blk * 2);
+          const uint32_t rr = live ? rbits | (rbits << 16) : 0u;
+          const BlockRef ref = make_block_ref(l1, c2, c3, (c4w >> (8 * side)) & 3u, as_h2(rr), ub);
+          // the key as an unevaluated sum hi + lo, coordinates in the order of the lookups: (4s, 4s+2), (4s+1, 4s+3)
+          __half2 h[8], l[8];
+          sub_block_hilo<0>(ref, t1, h[0], h[1], l[0], l[1]);
+          sub_block_hilo<1>(ref, t1, h[2], h[3], l[2], l[3]);
+          sub_block_hilo<2>(ref, t1, h[4], h[5], l[4], l[5]);
+          sub_block_hilo<3>(ref, t1, h[6], h[7], l[6], l[7]);
+          const uint32_t dst = sb + kPtKv + st * kPtStage + side * kPtKHalf + (i & 3) * 1024 + swz;
+          pt_sts128(dst, as_u32(h[0]), as_u32(h[1]), as_u32(h[2]), as_u32(h[3]));
+          pt_sts128(dst ^ 16u, as_u32(h[4]), as_u32(h[5]), as_u32(h[6]), as_u32(h[7]));
+          pt_sts128(dst + kPtKLo, as_u32(l[0]), as_u32(l[1]), as_u32(l[2]), as_u32(l[3]));
+          pt_sts128((dst + kPtKLo) ^ 16u, as_u32(l[4]), as_u32(l[5]), as_u32(l[6]), as_u32(l[7]));
         }
-        const uint32_t dst = sb + kPtKv + st * kPtStage + kPtKTile + (i & 7) * 1024 + swz;
-        pt_sts128(dst, w[0], w[1], w[2], w[3]);
-        pt_sts128(dst ^ 16u, w[4], w[5], w[6], w[7]);
+      } else {
+        const int blk = 4 * (int)crank + bi;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int tok = 8 * ((i & 3) + 4 * e) + t8;
+          const bool live = (jb0 + jb) * kTokenBlock + tok < len;
+          const uint32_t l1 = lds32(raw + tok * 32 + blk * 4);
+          const uint32_t c2 = lds8(raw + kO2 + tok * 8 + blk);
+          const uint32_t c3 = lds8(raw + kO3 + tok * 4 + (blk >> 1)) >> (4 * (bi & 1));
+          const uint32_t c4 = (lds16(raw + kO4 + tok * 2) >> (2 * blk)) & 3u;
+          const uint32_t rbits = lds16(raw + kORad + tok * 16 + blk * 2);
+          const uint32_t rr = live ? rbits | (rbits << 16) : 0u;
+          const BlockRef ref = make_block_ref(l1, c2, c3, c4, as_h2(rr), ub);
+          __half2 x[4], y[4];
+          sub_block_h2<0>(ref, t1, x[0], y[0]);
+          sub_block_h2<1>(ref, t1, x[1], y[1]);
+          sub_block_h2<2>(ref, t1, x[2], y[2]);
+          sub_block_h2<3>(ref, t1, x[3], y[3]);
+          // coordinates in natural order: (4s, 4s+1) = (x.lo, y.lo), (4s+2, 4s+3) = (x.hi, y.hi)
+          uint32_t w[8];
+#pragma unroll
+          for (int s = 0; s < 4; ++s) {
+            w[2 * s] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x5410);
+            w[2 * s + 1] = __byte_perm(as_u32(x[s]), as_u32(y[s]), 0x7632);
+          }
+          const uint32_t dst = sb + kPtKv + st * kPtStage + kPtKTile + ((i & 3) + 4 * e) * 1024 + swz;
+          pt_sts128(dst, w[0], w[1], w[2], w[3]);
+          pt_sts128(dst ^ 16u, w[4], w[5], w[6], w[7]);
+        }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();
@@ -331,25 +351,19 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         tc_commit_pair(sb + kPtBarS + 8 * t);
       }
     };
-    // Value MMAs go first when their P is ready (they free a stage for the decoders); the score MMAs run up to kPtScores - 1
-    // blocks ahead of them and keep the tensor core and the row owners busy.  Accumulator t is free for block jb once the
-    // value MMA of block jb - kPtScores, which reads P from its columns, has been issued (MMAs of one thread execute in order).
+    // A fixed order, so that the warp sleeps in its waits and leaves its scheduler to the others (looking at both barriers in turn cost a
+    // fifth of it): the score MMAs run kPtScores - 1 blocks ahead of the value MMAs.  Accumulator t is free for block jb once the value
+    // MMA of block jb - kPtScores, which reads P from its columns, has been issued (MMAs of one thread execute in order).
     bool ok = true;
-    int qk = 0, pv = 0, idle = 0;
-    while (pv < blocks && ok) {
-      if (pv < qk && __all_sync(0xffffffffu, tc_mbar_test(sb + kPtBarP + 8 * (pv % kPtScores), (uint32_t)(pv / kPtScores) & 1u))) {
-        issue_pv(pv++);
-        idle = 0;
-      } else if (qk < blocks && qk < pv + kPtScores &&
-                 __all_sync(0xffffffffu, tc_mbar_test(sb + kPtBarKv + 8 * (qk % kPtStages), (uint32_t)(qk / kPtStages) & 1u))) {
-        issue_qk(qk++);
-        idle = 0;
-      } else if (++idle > 32) {   // bounded like every wait
-        __nanosleep(32);
-        if (__any_sync(0xffffffffu, *abort_flag != 0) || idle > kTcSpin) {
-          *abort_flag = 1;
-          ok = false;
-        }
+    for (int jb = 1 - kPtScores; jb < blocks && ok; ++jb) {
+      if (jb >= 0) {
+        ok = __all_sync(0xffffffffu, tc_mbar_wait(sb + kPtBarP + 8 * (jb % kPtScores), (uint32_t)(jb / kPtScores) & 1u, abort_flag));
+        if (ok) issue_pv(jb);
+      }
+      const int qk = jb + kPtScores - 1;
+      if (ok && qk < blocks) {
+        ok = __all_sync(0xffffffffu, tc_mbar_wait(sb + kPtBarKv + 8 * (qk % kPtStages), (uint32_t)(qk / kPtStages) & 1u, abort_flag));
+        if (ok) issue_qk(qk);
       }
     }
     if (blocks > 0) {
