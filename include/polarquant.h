@@ -458,8 +458,8 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
  *
  * pq_prefix_attention: every one of n_queries queries attends (Eq. 3) to ALL cached tokens of one sequence of a packed cache
  * (paging == NULL: the contiguous cache of `capacity` tokens, else the paged cache and `capacity` is ignored).  A token is
- * decoded once for up to 32 or up to 256 (query, head) rows at head_dim 128, whichever is faster, and at other head_dims for
- * the heads of one query.
+ * decoded once for up to 256 (query, head) rows at head_dim 128 (for up to 32 or for one query's heads where that is faster),
+ * for up to 64 at other head_dims.
  *   q_dev, out_dev    [n_queries][n_q_heads][head_dim] of io_dtype; n_queries at most 65535
  *   cache_lens_dev    int32[cache_batch], the cache's; the queries see the cache_lens[sequence] tokens of `sequence`
  *   max_len           host-side upper bound on that length

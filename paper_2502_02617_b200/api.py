@@ -574,6 +574,8 @@ class PolarQuantCache:
             self._shared_ws, self._shared_need = {}, {}
         need = self._shared_need.get(args)
         if need is None:
+            if len(self._shared_need) >= 1024:   # of bounds that change with every call
+                self._shared_need.clear()
             need = self._shared_need[args] = size(self.d, *args)
         return _stream_workspace(self._shared_ws, need, stream, self.cache.device)
 
@@ -722,6 +724,8 @@ class PagedWindow:
     def _workspace(self, n_q, max_len, stream):
         need = self._need.get((n_q, max_len))
         if need is None:
+            if len(self._need) >= 1024:   # of bounds that change with every call
+                self._need.clear()
             need = self._need[n_q, max_len] = pq_window_workspace_bytes(self.d, self.batch, n_q, self.n_q_heads, self.n_kv_heads, max_len)
         if need <= self._unused.numel():   # one part: nothing is written
             return self._unused

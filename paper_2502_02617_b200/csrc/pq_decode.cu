@@ -118,6 +118,8 @@ __host__ inline RowCut cut_rows(int64_t all_rows) {
 
 struct DecodeArgs {
   int d, n_q_heads, n_kv_heads, batch, capacity, io_dtype, out_dtype;   // of q and of out
+  int early;   // of the persistent kernel: the kernel ahead in the stream (a window's attention) writes nothing that this one reads, and has every
+               // block say (launch_dependents) when all before it is done: wait for it at the end only
   int causal;  // 0: every query sees all tokens of its sequence (a prefix that the queries' own sequences share)
   int n_q;  // queries per sequence (1: decode).  `batch` counts (sequence, query) pairs: q and out are
             // [batch][n_q_heads][d] with pair p = sequence * n_q + query; `lens` and the cache are per sequence.
@@ -952,12 +954,10 @@ int64_t pq_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q_heads, i
   return std::max(std::max(cut, one), parts);
 }
 
-// Behind a kernel that has written the prefix's own result (shared->part_out): the window, and the merge of the two.
-static int32_t then_window(int32_t st, const pq::SharedPrefix* shared, int32_t* status, cudaStream_t stream) {
+// Behind the kernels that have written the prefix's own result (shared->part_out) and the window's: the merge of the two.
+static int32_t merge_with_window(int32_t st, const pq::SharedPrefix* shared, int32_t* status, cudaStream_t stream) {
   if (st != PQ_OK || shared == nullptr || shared->window == nullptr) return st;
   const pq::WindowArgs& w = shared->window->a;
-  st = pq::launch_window_call(*shared->window, false, stream);
-  if (st != PQ_OK) return st;
   return pq::launch_merge(w.d, w.n_rows, 2, shared->part_out, PQ_DTYPE_F32, shared->part_lse, shared->out, shared->out_dtype, nullptr, status, stream);
 }
 
@@ -982,7 +982,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   if (pairs > 65535 || n_kv_heads > 65535) return PQ_ERR_UNSUPPORTED;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(stream);
   pq::DecodeArgs a;
-  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.batch = (int)pairs; a.n_q = n_q; a.causal = causal; a.capacity = capacity;
+  a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.batch = (int)pairs; a.n_q = n_q; a.causal = causal; a.early = 0; a.capacity = capacity;
   a.io_dtype = io_dtype; a.out_dtype = !shared ? io_dtype : shared->window ? PQ_DTYPE_F32 : shared->out_dtype; a.scale = scale; a.S = S_dev; a.tables = reinterpret_cast<const pq::Tables*>(tables_dev);
   a.q = q_dev; a.cache = reinterpret_cast<const uint8_t*>(cache_dev); a.lens = cache_lens_dev; a.out = out_dev;
   a.status = status_dev;
@@ -993,13 +993,14 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
   const int g = n_q_heads / n_kv_heads;
   if (lse_dev != nullptr && n_q != 1 && causal) return PQ_ERR_UNSUPPORTED;
   pq::SplitCommon c;
-  c.d = head_dim; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = io_dtype; c.out_dtype = a.out_dtype; c.scale = scale;
+  c.d = head_dim; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = io_dtype; c.out_dtype = a.out_dtype; c.early = 0; c.scale = scale;
   c.S = S_dev; c.q = q_dev; c.out = out_dev; c.lse = lse_dev; c.status = status_dev;
   if (shared != nullptr && head_dim != 128) {
     static pq::DeviceMemo sm_count;
     const int n_sm = pq::sm_count_of_device(sm_count);
     if (n_sm == 0) return PQ_ERR_CUDA;
     const pq::PrefixCut cut = pq::cut_prefix(n_q, n_kv_heads, g, max_len, std::min(n_sm, pq::kFastMaxGridHost));
+    if ((int64_t)n_kv_heads * cut.row_blocks > 65535) return PQ_ERR_UNSUPPORTED;
     switch (head_dim) {
       case 16: return pq::launch_prefix<16>(a, *shared, workspace_dev, cut, st);
       case 32: return pq::launch_prefix<32>(a, *shared, workspace_dev, cut, st);
@@ -1039,8 +1040,15 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
       return pq::launch_prefix_tc(a, *shared, pq::prefix_tc_splits(n_q, n_kv_heads, g, max_len, n_sm), st);
     if (kernel == pq::kTensorKernel) return pq::launch_prefill_tc(a, batch, n_q, plan.n_splits, st);
     a.debug = fail_wait ? 1u : 0u;
+    if (shared != nullptr && shared->window != nullptr) {
+      // the window's blocks first: the cluster and the persistent kernel start beside them (12/12 heads, four queries over 362 compressed and
+      // 1548 recent tokens 24 -> 16 us; two over 25542 and 1647, 16/2 heads, 48 -> 46)
+      const int32_t first = pq::launch_window_call(*shared->window, false, st);
+      if (first != PQ_OK) return first;
+      a.early = c.early = 1;
+    }
     if (kernel == pq::kRowsKernel)
-      return then_window(pq::launch_rows_attention(a, pq::cut_rows((int64_t)n_q * g), batch, paged, st), shared, status_dev, st);
+      return merge_with_window(pq::launch_rows_attention(a, pq::cut_rows((int64_t)n_q * g), batch, paged, st), shared, status_dev, st);
     if (kernel == pq::kPersistentKernel) {
       a.epoch = pq::next_epoch();
       static pq::DeviceMemo configured[4];
@@ -1048,7 +1056,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
           g <= 4 ? (paged ? pq::decode_attention_fast_kernel<1, true> : pq::decode_attention_fast_kernel<1, false>)
                  : (paged ? pq::decode_attention_fast_kernel<2, true> : pq::decode_attention_fast_kernel<2, false>);
       if (pq::configure_for_device(fast, pq::kFsTotal, configured[(g > 4 ? 2 : 0) + (paged ? 1 : 0)]) == 0) return PQ_ERR_CUDA;
-      return then_window(pq::launch_persistent(fast, a, n_sm, pq::kFastThreads, pq::kFsTotal, st), shared, status_dev, st);
+      return merge_with_window(pq::launch_persistent(fast, a, n_sm, pq::kFastThreads, pq::kFsTotal, st), shared, status_dev, st);
     }
   }
   switch (head_dim) {
@@ -1063,7 +1071,7 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
       return pq::dispatch_split_attention(pq::packed_split<64, true>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st);
     }
     default:
-      return then_window(pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st),
+      return merge_with_window(pq::dispatch_split_attention(pq::packed_split<128>(c, n_q, causal, a.tables, a.cache, cache_lens_dev, pg), pairs, max_len, st),
                          shared, status_dev, st);
   }
 }
@@ -1275,9 +1283,7 @@ int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, 
   if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
   if (batch <= 0 || n_q <= 0 || n_q_heads <= 0 || n_kv_heads <= 0 || max_len <= 0 || n_q_heads % n_kv_heads) return PQ_ERR_INVALID_ARG;
   const int64_t rows = (int64_t)batch * n_q * n_q_heads;
-  int64_t parts = 1;   // of the kernel that cuts more
-  for (int32_t dtype : {PQ_DTYPE_F32, PQ_DTYPE_BF16})
-    parts = std::max<int64_t>(parts, pq::window_cut(head_dim, dtype, batch, n_q, n_kv_heads, n_q_heads / n_kv_heads, max_len, pq::kFastMaxGridHost).parts);
+  const int64_t parts = pq::window_most_parts(head_dim, batch, n_q, n_kv_heads, n_q_heads / n_kv_heads, max_len);
   return parts > 1 ? parts * rows * (head_dim + 1) * 4 : 16;
 }
 
@@ -1296,9 +1302,9 @@ static int32_t window_call(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_hea
   if (((uintptr_t)q_dev | (uintptr_t)pool_dev | (uintptr_t)out_dev | (uintptr_t)workspace_dev) & 15) return PQ_ERR_ALIGNMENT;
   if (((uintptr_t)window_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
   const int g = n_q_heads / n_kv_heads;
-  const pq::WindowRows rows = pq::window_rows(head_dim, kv_dtype, n_q, g);
+  const pq::WindowRows rows = pq::window_rows(head_dim, kv_dtype, batch, n_q, n_kv_heads, g, max_len);
   if (batch > 65535 || n_kv_heads * rows.blocks > 65535) return PQ_ERR_UNSUPPORTED;
-  call->kv_dtype = kv_dtype; call->rows = rows.rows; call->batch = batch; call->max_len = max_len;
+  call->kv_dtype = kv_dtype; call->rows = rows; call->batch = batch; call->max_len = max_len;
   a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.early = 0;
   a.row_blocks = (int)rows.blocks; a.n_parts = 1; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;
   a.q = q_dev; a.pool = reinterpret_cast<const uint8_t*>(pool_dev); a.lens = window_lens_dev; a.out = out_dev; a.lse = lse_dev;

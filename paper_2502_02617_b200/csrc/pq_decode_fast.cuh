@@ -687,7 +687,7 @@ __global__ void __launch_bounds__(kFastThreads, 1) decode_attention_fast_kernel(
       for (int e = 0; e < 4; ++e) s_col[4 * i + e] = ld_const_now(a.S + (16 * i + rot_k + e) * 128 + rot_j);
   };
   if (kHG == 1) load_s_col();   // two groups: held through the work split, the 32 registers spill
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  if (!a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
   __syncthreads();
 
   const int n_units = a.batch * a.n_kv_heads, cta = blockIdx.x;   // the work split: see list_segments
@@ -1123,6 +1123,7 @@ __global__ void __launch_bounds__(kFastThreads, 1) decode_attention_fast_kernel(
   }
   }
   if (tid == 0 && *abort_flag) set_status(a.status, PQ_ERR_TIMEOUT);
+  if (a.early) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 }  // namespace pq

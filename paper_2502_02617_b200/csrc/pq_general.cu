@@ -353,7 +353,7 @@ int32_t pq_general_decode_attention(const pq_general_config* cfg, int32_t n_q_he
   if (io_dtype != PQ_DTYPE_F32 && io_dtype != PQ_DTYPE_BF16) return PQ_ERR_UNSUPPORTED;
   if (((uintptr_t)centroids_dev & 7) || ((uintptr_t)cache_dev & 1)) return PQ_ERR_ALIGNMENT;
   pq::SplitCommon c;
-  c.d = g.d; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = c.out_dtype = io_dtype; c.scale = scale;
+  c.d = g.d; c.n_q_heads = n_q_heads; c.n_kv_heads = n_kv_heads; c.io_dtype = c.out_dtype = io_dtype; c.early = 0; c.scale = scale;
   c.S = S_dev; c.q = q_dev; c.out = out_dev; c.lse = nullptr; c.status = status_dev;
   return pq::launch_gen_attention(g, c, batch, capacity, centroids_dev, cache_dev, cache_lens_dev,
                                   reinterpret_cast<cudaStream_t>(stream));

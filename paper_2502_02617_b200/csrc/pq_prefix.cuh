@@ -1,5 +1,5 @@
-// Attention of many queries over one compressed sequence that all of them see (a shared prefix), any head_dim of the packed cache,
-// for up to a few dozen (query, head) rows per kv head (included by pq_decode.cu; more rows of 128 take prefill_tc_kernel).
+// Attention of many queries over one compressed sequence that all of them see (a shared prefix): the kernel for head_dims below 128, and
+// the rotations before and after it and prefix_tc_kernel (included by pq_decode.cu).
 //
 // prefix_mma_kernel: a block of eight warps takes 16 kTiles rows of a kv head and a range of the tokens.  kTiles warps share a
 // stream of tiles of 16 kTiles tokens; 8 / kTiles streams share the range.  Each warp of a stream decodes 16 tokens of a tile
@@ -8,9 +8,11 @@
 // 16 rows with all tokens of the tile (mma.sync): S = Q'lo K_hi + Q'hi K_lo + Q'hi K_hi with the queries rotated, scaled and split
 // the same way before, and O += P V with weights of fp16, whose sum is taken of what the product sees.  The packed codes of a
 // stream's next tile are in registers while the present one is decoded and multiplied.  A level's table is at most 16 pairs of
-// (cos, sin), 128 bytes: lookups are free of bank conflicts without copies.
-// The streams meet in shared memory, the blocks of a cluster in each other's, and the parts beyond that in the kernel that
-// rotates back (merge_unrotate_kernel, or prefix_unrotate_kernel below 128).
+// (cos, sin), 128 bytes: lookups are free of bank conflicts without copies, but two wavefronts each, and shared memory bounds
+// the kernel (34 wavefronts per token and kv head at head_dim 128, where the kernels with larger, replicated tables are faster: 16 rows
+// over 32768 tokens 57 us against 49).  The streams meet in shared memory, the blocks of a cluster in each other's, and the parts beyond
+// that in prefix_unrotate_kernel.
+// Measured, 16/8 heads of 64: 16 queries over 4096 tokens 19 us, 64 over 8192 59 (a decode per query took 36 us for the former).
 #pragma once
 
 namespace pq {
@@ -49,15 +51,7 @@ __device__ __forceinline__ void px_load(PxCodes<D>& c, const uint8_t* tb, int to
   constexpr int kNb = D / 16, kB1 = 4 * kNb, kB2 = kNb, kB3 = kNb >= 2 ? kNb / 2 : 1, kB4 = kNb >= 4 ? kNb / 4 : 1, kBr = 2 * kNb;
   constexpr int o2 = kTokenBlock * kB1, o3 = o2 + kTokenBlock * kB2, o4 = o3 + kTokenBlock * kB3, orad = o4 + kTokenBlock * kB4;
   const uint8_t *p1 = tb + tok * kB1, *p2 = tb + o2 + tok * kB2, *p3 = tb + o3 + tok * kB3, *p4 = tb + o4 + tok * kB4, *pr = tb + orad + tok * kBr;
-  if constexpr (D == 128) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p1 + 16 * half);
-    c.l1[0] = w.x; c.l1[1] = w.y; c.l1[2] = w.z; c.l1[3] = w.w;
-    c.l2 = *reinterpret_cast<const uint32_t*>(p2 + 4 * half);
-    c.l3 = *reinterpret_cast<const uint16_t*>(p3 + 2 * half);
-    c.l4 = p4[half];
-    const uint2 r = *reinterpret_cast<const uint2*>(pr + 8 * half);
-    c.r[0] = r.x; c.r[1] = r.y;
-  } else if constexpr (D == 64) {
+  if constexpr (D == 64) {
     const uint2 w = *reinterpret_cast<const uint2*>(p1 + 8 * half);
     c.l1[0] = w.x; c.l1[1] = w.y;
     c.l2 = *reinterpret_cast<const uint16_t*>(p2 + 2 * half);

@@ -38,6 +38,7 @@ constexpr int kUnitStride = 20;            // floats between the 16-coordinate g
 // What the kernel needs beside the layout.
 struct SplitCommon {
   int d, n_q_heads, n_kv_heads, io_dtype, out_dtype;
+  int early;   // as in DecodeArgs
   int tile, stage_bytes;   // tokens of a tile, bytes of its staged keys (or values): set by dispatch_split_attention
   float scale;
   const float* S;
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(32 * split_warps(kH), 1) split_attention_kerne
   split_commit();
   if (P::kEarlyTables) p.fill_tables(tab, tid);
   if constexpr (P::kPairs) p.fill_pairs(pairs, tid, kSplitThreads);
-  asm volatile("griddepcontrol.wait;" ::: "memory");   // lengths, cache and queries may come from the kernel before this one
+  if (!c.early) asm volatile("griddepcontrol.wait;" ::: "memory");   // lengths, cache and queries may come from the kernel before this one
   const int64_t q0 = ((int64_t)pair * c.n_q_heads + hk * grp) * d;
   const int len = p.len(pair);
   for (int i = tid; i < kH * dp; i += kSplitThreads) {
@@ -460,6 +461,7 @@ __global__ void __launch_bounds__(32 * split_warps(kH), 1) split_attention_kerne
     }
   }
   if (C > 1) cluster_wait();
+  if (c.early) asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // Clusters of 2^log2c blocks that the device holds at once, one block per SM: a cluster lies inside a GPC, whose SMs need not be

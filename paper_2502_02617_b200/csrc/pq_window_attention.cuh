@@ -179,8 +179,8 @@ __device__ __forceinline__ void window_finish(const WindowArgs& a, const float* 
 }
 __device__ __forceinline__ void window_begin(const WindowArgs& a) {
   if (!a.early) {
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // behind the wait: see DecodeArgs::early
   }
 }
 

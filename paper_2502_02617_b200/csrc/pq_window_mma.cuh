@@ -1,6 +1,6 @@
 // Attention over the paged window on tensor cores: bf16 rows of 64 or 128 (included by pq_decode.cu).
 //
-// A block of four warps takes 16 kTiles (query, head) rows of a kv head and a range of the window's tokens.  kTiles warps, each
+// A block of four warps takes 16 kTiles (query, head) rows of a kv head and a range of the window's tokens.  kTiles (1 or 4) warps, each
 // with 16 rows, share a stream of 16-token tiles; 4 / kTiles streams share the range.  A stream copies its tiles with 16-byte
 // cp.async into a ring of its own, keys and values of a tile as one piece each, 16-byte chunk x of row t at x ^ (t & 7).
 //   scores (rows x tokens) = Q (16 x D) K^T: bf16 queries as they are, float32 ones as three bf16 terms (24 bits)
@@ -289,9 +289,7 @@ static int32_t launch_window_mma_as(const WindowArgs& a, int batch, const Window
 }
 template <int D, int kQTerms>
 static int32_t launch_window_mma_rows(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
-  return rows == 16   ? launch_window_mma_as<D, kQTerms, 1>(a, batch, cut, stream)
-         : rows == 32 ? launch_window_mma_as<D, kQTerms, 2>(a, batch, cut, stream)
-                      : launch_window_mma_as<D, kQTerms, 4>(a, batch, cut, stream);
+  return rows == 16 ? launch_window_mma_as<D, kQTerms, 1>(a, batch, cut, stream) : launch_window_mma_as<D, kQTerms, 4>(a, batch, cut, stream);
 }
 
 // Which kernel takes a call, the (query, head) rows of its blocks for `all` rows of a kv head, and the streams of tokens in a block.
@@ -300,22 +298,27 @@ struct WindowRows {
   int rows, streams;
   int64_t blocks;
 };
-static WindowRows window_rows(int d, int kv_dtype, int n_q, int g) {
-  const int64_t all = (int64_t)n_q * g;
-  WindowRows r;
-  if (window_on_tensor_cores(d, kv_dtype)) {
-    r.rows = all <= 16 ? 16 : all <= 32 ? 32 : 64;
-    r.streams = 64 / r.rows;
-  } else {
-    r.rows = all == 1 ? 1 : all == 2 ? 2 : 4;
-    r.streams = kWinWarps;
-  }
-  r.blocks = (all + r.rows - 1) / r.rows;
+static WindowRows window_rows_of(int rows, int streams, int64_t all) {
+  WindowRows r = {rows, streams, (all + rows - 1) / rows};
   return r;
 }
-static WindowCut window_cut(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len, int n_sm) {
-  const WindowRows r = window_rows(d, kv_dtype, n_q, g);
-  return cut_window(batch * n_kv_heads * r.blocks, max_len, n_sm, r.streams);
+// On tensor cores 16 rows and four streams are as fast as 64 and one (the blocks that share a window's tokens find them in L2), or faster where
+// that leaves no rows empty and needs no parts: 35 rows over 2048 tokens 23.0 and 24.5 us, 32 over 2000 15.3 and 17.3 (32 rows and two
+// streams), 64 over 4000 25.4 and 31.6, 64 over 2048 of 32 sequences 132 both.  With more than 48 rows over windows larger than L2 one
+// reading is: eight sequences of 8192 138 and 115.
+static WindowRows window_rows(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len) {
+  const int64_t all = (int64_t)n_q * g;
+  if (!window_on_tensor_cores(d, kv_dtype)) return window_rows_of(all == 1 ? 1 : all == 2 ? 2 : 4, kWinWarps, all);
+  const bool once = all > 48 && (double)batch * n_kv_heads * max_len * (4 * d) > 126e6;
+  return once ? window_rows_of(64, 1, all) : window_rows_of(16, kWinWarps, all);
+}
+// Parts that a call may leave: of either way to take the rows, so that a smaller bound on the length never needs more.
+static int window_most_parts(int d, int batch, int n_q, int n_kv_heads, int g, int max_len) {
+  const int64_t all = (int64_t)n_q * g, heads = (int64_t)batch * n_kv_heads;
+  int parts = 1;
+  for (const WindowRows& r : {window_rows_of(all == 1 ? 1 : all == 2 ? 2 : 4, kWinWarps, all), window_rows_of(16, kWinWarps, all), window_rows_of(64, 1, all)})
+    parts = std::max(parts, cut_window(heads * r.blocks, max_len, kFastMaxGridHost, r.streams).parts);
+  return parts;
 }
 static int32_t launch_window_attention(const WindowArgs& a, int kv_dtype, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
   const bool exact = a.io_dtype == PQ_DTYPE_BF16;   // queries that are one bf16 term
@@ -336,18 +339,19 @@ static int32_t launch_window_attention(const WindowArgs& a, int kv_dtype, int ro
 // An attention over a window with its arguments checked, and its launch: its parts, where there are several, lie at a.part_out.
 struct WindowCall {
   WindowArgs a;
-  int kv_dtype, rows, batch, max_len;
+  WindowRows rows;
+  int kv_dtype, batch, max_len;
 };
 static int32_t launch_window_call(const WindowCall& w, bool early, cudaStream_t stream) {
   static DeviceMemo sm_count;
   const int n_sm = sm_count_of_device(sm_count);
   if (n_sm == 0) return PQ_ERR_CUDA;
   WindowArgs a = w.a;
-  const WindowCut cut = window_cut(a.d, w.kv_dtype, w.batch, a.n_q, a.n_kv_heads, a.n_q_heads / a.n_kv_heads, w.max_len, std::min(n_sm, kFastMaxGridHost));
+  const WindowCut cut = cut_window((int64_t)w.batch * a.n_kv_heads * w.rows.blocks, w.max_len, std::min(n_sm, kFastMaxGridHost), w.rows.streams);
   a.early = early;
   a.n_parts = cut.parts;
   a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * a.d : 0);
-  const int32_t st = launch_window_attention(a, w.kv_dtype, w.rows, w.batch, cut, stream);
+  const int32_t st = launch_window_attention(a, w.kv_dtype, w.rows.rows, w.batch, cut, stream);
   if (st != PQ_OK || cut.parts == 1) return st;
   // the window kernel has reported the rows that see nothing
   return launch_merge(a.d, a.n_rows, cut.parts, a.part_out, PQ_DTYPE_F32, a.part_lse, a.out, a.out_dtype, a.lse, nullptr, stream);

@@ -265,6 +265,48 @@ def test_shared_attention_on_two_streams():
     assert all(torch.equal(x, want[i]) for i in range(2) for x in got[i])
 
 
+def test_two_captured_graphs_do_not_share_what_they_write_between():
+    """Two graphs of the same calls, captured one after the other and replayed at once on two streams."""
+    cache = make_cache([5000], 8, 2, 128)
+    w = pq.PagedWindow(4, 8, 2, 128, 64, 128, torch.arange(128).view(4, 32), device=DEV)
+    fill_window(w, [2000] * 4, 3)
+    qs = [synthetic.queries(i, 4, 8, 128, BF16, DEV) for i in range(2)]
+    want = [(cache.attend_shared(q, w), cache.attend_prefix(q), w.attend(q)) for q in qs]
+    graphs, outs, streams = [], [], [torch.cuda.Stream() for _ in qs]
+    for q in qs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append((cache.attend_shared(q, w), cache.attend_prefix(q), w.attend(q)))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for got, wanted in zip(outs, want) for a, b in zip(got, wanted))
+
+
+def test_a_serving_step_under_a_stream_of_its_own():
+    """Everything on a side stream while the current one is busy with something else."""
+    B, hq, hkv, d = 3, 8, 2, 128
+    cache = make_cache([700], hq, hkv, d)
+    offsets = cache.lens.repeat(B)
+    side = torch.cuda.Stream()
+    results = []
+    for stream in (None, side):
+        w = pq.PagedWindow(B, hq, hkv, d, 16, 6, torch.arange(6).view(B, 2), frequencies=pq.pq_rotary_frequencies(d), device=DEV)
+        w.pool.zero_()
+        g = torch.Generator(DEV).manual_seed(1)
+        q, k, v = (torch.randn((B, h, d), generator=g, device=DEV).to(BF16) for h in (hq, hkv, hkv))
+        torch.cuda.synchronize()
+        if stream is not None:
+            torch.empty(1 << 26, device=DEV).normal_()
+        out = cache.attend_shared(w.append(q, k, v, offsets=offsets, stream=stream), w, stream=stream)
+        torch.cuda.synchronize()
+        results.append((out.clone(), w.pool.clone(), w.lens.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+
+
 def test_refusals():
     cache = make_cache([100], 8, 2, 128)
     w = pq.PagedWindow(4, 8, 2, 128, 16, 16, torch.arange(16).view(4, 4), device=DEV)
