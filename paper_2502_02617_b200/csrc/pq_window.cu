@@ -29,7 +29,7 @@ __device__ __forceinline__ bool append_fits(const AppendArgs& a, int base, int c
   return base >= 0 && (int64_t)base + count <= (int64_t)a.pg.page_tokens * a.pg.pages_per_seq;
 }
 __device__ __forceinline__ int64_t append_target(const AppendArgs& a, int seq, int base, int count, int place) {
-  if (!append_fits(a, base, count) || (unsigned)(place - base) >= (unsigned)count) {
+  if (!append_fits(a, base, count) || place < base || place - base >= count) {   // ends that do not rise leave rows before their sequence
     set_status(a.status, PQ_ERR_CAPACITY);
     return -1;
   }

@@ -215,6 +215,25 @@ def test_append_reports_what_does_not_fit():
             w.check_status()
 
 
+@pytest.mark.parametrize("d,rotary", [(64, 64), (16, 6)])   # rows as 16-byte pieces, and pair by pair
+@pytest.mark.parametrize("ends", [[0, 60, 30, 5, 60], [0, 60, -7, 60, 60], [0, 40, 20, 200, 60]])
+def test_ends_that_do_not_rise_write_into_no_other_sequence(ends, d, rotary):
+    """cu_seqlens that fall, or lie beyond the rows: rows may be refused, but nothing outside the sequences' own pages changes."""
+    B, hq, hkv, P, n = 4, 2, 1, 16, 60
+    w = make_window(B, hq, hkv, d, P, 128, frequencies=pq.pq_rotary_frequencies(rotary), seed=4)
+    own = w.page_table.clone()
+    g = torch.Generator(DEV).manual_seed(7)
+    q, k, v = (torch.randn((n, h, d), generator=g, device=DEV).to(BF16) for h in (hq, hkv, hkv))
+    pool = w.pool.clone()
+    w.append(q, k, v, torch.tensor(ends, dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    lens = w.lens.cpu().tolist()
+    assert all(0 <= m <= max(0, b - a) for m, a, b in zip(lens, ends, ends[1:])), lens
+    assert torch.equal(w.page_table, own)
+    for page in set(range(w.n_pages)) - set(own.flatten().tolist()):
+        assert torch.equal(w.pool[page], pool[page])
+
+
 def test_append_refuses_tensors_that_do_not_fit():
     w = make_window(2, 4, 2, 64, 16, 32, frequencies=pq.pq_rotary_frequencies(64))
     ok = dict(q=torch.zeros((2, 4, 64), dtype=BF16, device=DEV), k=torch.zeros((2, 2, 64), dtype=BF16, device=DEV), v=torch.zeros((2, 2, 64), dtype=BF16, device=DEV))
