@@ -7,8 +7,9 @@
 // halves the values with every step (kVals values over kLanes lanes cost kVals - 1 shuffles, and each lane ends with one
 // score).  The streams meet at the end: groups by shuffles, warps in shared memory, the blocks of a cluster in each other's
 // shared memory, and the parts beyond a cluster in merge_attention_kernel.  Everything is float32 on the values as they are.
-// bf16 rows of 64 and 128 are faster on tensor cores (pq_window_mma.cuh).  Bound by issue and the latency of its loads: 16 sequences of 2000
-// float32 tokens, 32/8 heads of 128, 56 us (4.7 TB/s); in bf16, 64 of up to 4096 tokens, it took 193 us against 111 there.
+// bf16 rows of 64 and 128 are faster on tensor cores (pq_window_mma.cuh).  Bound by issue and the latency of its loads: float32
+// windows of 32/8 heads of 128, 16 sequences of 2000 tokens 56 us (4.7 TB/s), one of 4000 18.8, six queries each on four of 2000 53.6 (93 in
+// rows of four); in bf16, 64 sequences of up to 4096 tokens, it took 193 us against 111 there.
 #pragma once
 
 #include "pq_window_common.cuh"
@@ -446,13 +447,15 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
 struct WindowCut {
   int cluster, parts;
 };
-static WindowCut cut_window(int64_t units, int max_len, int n_sm, int streams) {
+// `steps`: of a stream for a tile (float32 rows of 128 are read four tokens at a time, of 64 eight), each as long as a tile's otherwise.  Counted
+// as tiles a float32 window of 4000 tokens stayed in one cluster: 43.6 us, 18.8 in parts.
+static WindowCut cut_window(int64_t units, int max_len, int n_sm, int streams, int steps) {
   const int64_t tiles = ((int64_t)max_len + 15) / 16, one_wave = std::max<int64_t>(1, 4 * (int64_t)n_sm / units);
   const int64_t splits = std::min(std::max<int64_t>(1, tiles / 2), std::max(one_wave, tiles / (16 * streams)));
   WindowCut c = {1, 1};
   while (c.cluster < kWinMaxCluster && 2 * c.cluster <= splits) c.cluster *= 2;
   if (c.cluster == kWinMaxCluster)
-    c.parts = (int)std::max<int64_t>(1, std::min({(tiles + 64 * streams - 1) / (64 * streams), one_wave / kWinMaxCluster, (int64_t)kWinMaxParts}));
+    c.parts = (int)std::max<int64_t>(1, std::min({(tiles * steps + 64 * streams - 1) / (64 * streams), one_wave / kWinMaxCluster, (int64_t)kWinMaxParts}));
   return c;
 }
 
@@ -481,7 +484,10 @@ static int32_t launch_window(void (*kernel)(WindowArgs), const WindowArgs& a, in
 }
 template <class T, int D>
 static int32_t launch_window_rows(const WindowArgs& a, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
-  return launch_window(rows == 1 ? window_attention_kernel<T, D, 1> : rows == 2 ? window_attention_kernel<T, D, 2> : window_attention_kernel<T, D, 4>, a, batch,
-                       cut, 0, stream);
+  return launch_window(rows == 1   ? window_attention_kernel<T, D, 1>
+                       : rows == 2 ? window_attention_kernel<T, D, 2>
+                       : rows == 4 ? window_attention_kernel<T, D, 4>
+                                   : window_attention_kernel<T, D, 8>,
+                       a, batch, cut, 0, stream);
 }
 }  // namespace pq

@@ -295,12 +295,15 @@ static int32_t launch_window_mma_rows(const WindowArgs& a, int rows, int batch, 
 // Which kernel takes a call, the (query, head) rows of its blocks for `all` rows of a kv head, and the streams of tokens in a block.
 static bool window_on_tensor_cores(int d, int kv_dtype) { return kv_dtype == PQ_DTYPE_BF16 && d >= 64; }
 struct WindowRows {
-  int rows, streams;
+  int rows, streams, steps;
   int64_t blocks;
 };
-static WindowRows window_rows_of(int rows, int streams, int64_t all) {
-  WindowRows r = {rows, streams, (all + rows - 1) / rows};
+static WindowRows window_rows_of(int rows, int streams, int steps, int64_t all) {
+  WindowRows r = {rows, streams, steps, (all + rows - 1) / rows};
   return r;
+}
+static WindowRows window_rows_of_lanes(int d, int kv_dtype, int64_t all) {
+  return window_rows_of(all == 1 ? 1 : all == 2 ? 2 : all <= 4 ? 4 : 8, kWinWarps, kv_dtype == PQ_DTYPE_F32 && d >= 64 ? d / 32 : 1, all);
 }
 // On tensor cores 16 rows and four streams are as fast as 64 and one (the blocks that share a window's tokens find them in L2), or faster where
 // that leaves no rows empty and needs no parts: 35 rows over 2048 tokens 23.0 and 24.5 us, 32 over 2000 15.3 and 17.3 (32 rows and two
@@ -308,16 +311,17 @@ static WindowRows window_rows_of(int rows, int streams, int64_t all) {
 // reading is: eight sequences of 8192 138 and 115.
 static WindowRows window_rows(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len) {
   const int64_t all = (int64_t)n_q * g;
-  if (!window_on_tensor_cores(d, kv_dtype)) return window_rows_of(all == 1 ? 1 : all == 2 ? 2 : 4, kWinWarps, all);
+  if (!window_on_tensor_cores(d, kv_dtype)) return window_rows_of_lanes(d, kv_dtype, all);
   const bool once = all > 48 && (double)batch * n_kv_heads * max_len * (4 * d) > 126e6;
-  return once ? window_rows_of(64, 1, all) : window_rows_of(16, kWinWarps, all);
+  return once ? window_rows_of(64, 1, 1, all) : window_rows_of(16, kWinWarps, 1, all);
 }
 // Parts that a call may leave: of either way to take the rows, so that a smaller bound on the length never needs more.
 static int window_most_parts(int d, int batch, int n_q, int n_kv_heads, int g, int max_len) {
   const int64_t all = (int64_t)n_q * g, heads = (int64_t)batch * n_kv_heads;
   int parts = 1;
-  for (const WindowRows& r : {window_rows_of(all == 1 ? 1 : all == 2 ? 2 : 4, kWinWarps, all), window_rows_of(16, kWinWarps, all), window_rows_of(64, 1, all)})
-    parts = std::max(parts, cut_window(heads * r.blocks, max_len, kFastMaxGridHost, r.streams).parts);
+  for (const WindowRows& r : {window_rows_of_lanes(d, PQ_DTYPE_F32, all), window_rows_of_lanes(d, PQ_DTYPE_BF16, all), window_rows_of(16, kWinWarps, 1, all),
+                              window_rows_of(64, 1, 1, all)})
+    parts = std::max(parts, cut_window(heads * r.blocks, max_len, kFastMaxGridHost, r.streams, r.steps).parts);
   return parts;
 }
 static int32_t launch_window_attention(const WindowArgs& a, int kv_dtype, int rows, int batch, const WindowCut& cut, cudaStream_t stream) {
@@ -347,7 +351,8 @@ static int32_t launch_window_call(const WindowCall& w, bool early, cudaStream_t 
   const int n_sm = sm_count_of_device(sm_count);
   if (n_sm == 0) return PQ_ERR_CUDA;
   WindowArgs a = w.a;
-  const WindowCut cut = cut_window((int64_t)w.batch * a.n_kv_heads * w.rows.blocks, w.max_len, std::min(n_sm, kFastMaxGridHost), w.rows.streams);
+  const WindowCut cut = cut_window((int64_t)w.batch * a.n_kv_heads * w.rows.blocks, w.max_len, std::min(n_sm, kFastMaxGridHost), w.rows.streams,
+                                   w.rows.steps);
   a.early = early;
   a.n_parts = cut.parts;
   a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * a.d : 0);
