@@ -10,10 +10,10 @@
 //   * warps 0-7 (row owners): thread = row and half of a block's tokens.  A row's two threads exchange their maxima through shared memory
 //     and one barrier of the eight warps, take the same lazy reference, and write 16 columns of P each.  80 registers a thread
 //     are enough for half a row, so that 24 warps fit where 16 do with a whole row.
-// Bound by instruction issue: 0.93 us per block of a pair (prefill_tc_kernel 1.0), 4900 warp instructions per CTA; without the lookups
-// 0.84, without the exponentials 0.82, without both 0.69, and with a third of the score MMAs as well 0.62.  A CTA alone with 128 rows,
-// whole blocks and two stages takes 1.5 us a block and is faster nowhere.  Measured with the rotations, 32/8 heads: 64 queries over 32768
-// tokens 84 us, over 65536 136; 256 over 32768 275.
+// Bound by instruction issue and the latency of the lookups: 0.93 us per block of a pair at first (prefill_tc_kernel 1.0) with 4900 warp
+// instructions per CTA, now about 4000; then, without the lookups 0.84, without the exponentials 0.82, without both 0.69, and with a third of the
+// score MMAs as well 0.62.  A CTA alone with 128 rows, whole blocks and two stages takes 1.5 us a block and is faster nowhere.  Measured with the
+// rotations, 32/8 heads: 64 queries over 32768 tokens 74 to 76 us (90 in prefill_tc_kernel); the kernel alone 71 with caches cold, its MMAs 56 % of that.
 #pragma once
 
 #include "pq_tc_common.cuh"
