@@ -416,6 +416,7 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  *                      h*q_head_stride + i, of k and v at t*kv_token_stride + h*kv_head_stride + i (strides in elements; the
  *                      three may be parts of one projection's rows).  q_dev = NULL: no queries (n_q_heads = 0, q_out = NULL).
  *                      Unlike other device pointers these three, and q_out, need only their element's alignment
+ *                      and may be NULL where total_tokens = 0, a call that does nothing
  *   q_out_dev          [total_tokens][n_q_heads][head_dim] contiguous; may be q_dev where q is laid out so
  *   cu_seqlens_dev     int32[batch+1] as for pq_encode_kv, but rows behind cu[batch] are allowed (a padded batch) and give
  *                      nothing: neither the window nor q_out is written for them; NULL: row b is sequence b's (total_tokens = batch)

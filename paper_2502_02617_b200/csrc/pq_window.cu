@@ -332,9 +332,9 @@ int32_t pq_append_window(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_heads
                          const pq_paging* paging, int32_t* status_dev, void* stream) {
   pq::NvtxRange nvtx_range("pq_append_window");
   if (!pq::window_head_dim(head_dim) || (dtype != PQ_DTYPE_F32 && dtype != PQ_DTYPE_BF16)) return PQ_ERR_UNSUPPORTED;
-  if (!k_dev || !v_dev || !pool_dev || !window_lens_dev || !status_dev) return PQ_ERR_INVALID_ARG;
+  if (!pool_dev || !window_lens_dev || !status_dev || (total_tokens != 0 && (!k_dev || !v_dev))) return PQ_ERR_INVALID_ARG;
   if (batch <= 0 || total_tokens < 0 || n_kv_heads <= 0 || n_q_heads < 0) return PQ_ERR_INVALID_ARG;
-  if ((q_dev != nullptr) != (n_q_heads > 0) || (q_out_dev != nullptr) != (n_q_heads > 0)) return PQ_ERR_INVALID_ARG;
+  if (total_tokens > 0 && ((q_dev != nullptr) != (n_q_heads > 0) || (q_out_dev != nullptr) != (n_q_heads > 0))) return PQ_ERR_INVALID_ARG;
   if (!cu_seqlens_dev && total_tokens != batch) return PQ_ERR_INVALID_ARG;
   if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 2 || (rotary_dim > 0) != (frequencies_dev != nullptr)) return PQ_ERR_INVALID_ARG;
   if (q_token_stride < 0 || q_head_stride < 0 || kv_token_stride < 0 || kv_head_stride < 0) return PQ_ERR_INVALID_ARG;

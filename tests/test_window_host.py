@@ -71,6 +71,12 @@ def test_bad_paging_is_refused(pg, status):
     assert append(pg=pg) == status and attend(pg=pg) == status
 
 
+def test_an_append_of_no_rows_does_nothing():
+    assert append(total=0, cu=GOOD, q=None, k=None, v=None, q_out=None) == pq.OK
+    assert append(total=0, cu=GOOD) == pq.OK
+    assert append(total=0, cu=GOOD, lens=None) == pq.ERR_INVALID_ARG and append(total=0) == pq.ERR_INVALID_ARG
+
+
 def test_missing_paging_is_refused():
     args = [64, 4, 2, GOOD, pq.DTYPE_BF16, GOOD, pq.DTYPE_BF16, GOOD, 2, 1, None, 64, 0.1, GOOD, None, GOOD, GOOD, None]
     assert L.pq_window_attention(*args) == pq.ERR_INVALID_ARG
