@@ -201,10 +201,15 @@ def _stream_workspace(kept: dict, need: int, stream, device):
     has its own.  A capture takes a new one from the graph's pool every time: calls outside must not share it with a replay."""
     key = (_native or native()).current_stream(device.index) if stream is None else stream.cuda_stream
     ws = kept.get(key)
-    if ws is None or ws.numel() < need or torch.cuda.is_current_stream_capturing():
+    if stream is None:
+        capturing = torch.cuda.is_current_stream_capturing()
+    else:
+        with _on(stream, device):   # whichever is current outside
+            capturing = torch.cuda.is_current_stream_capturing()
+    if ws is None or ws.numel() < need or capturing:
         with _on(stream, device):
             ws = torch.empty(need, dtype=torch.uint8, device=device)
-        if not torch.cuda.is_current_stream_capturing():
+        if not capturing:
             while len(kept) >= 8 and key not in kept:   # of streams that are no longer used
                 kept.pop(next(iter(kept)))
             kept[key] = ws

@@ -402,6 +402,38 @@ def test_append_and_attend_in_a_captured_graph():
     assert w.lens.cpu().tolist() == [8] * B and torch.equal(w.pool, eager.pool) and w.check_status()[0] == 0
 
 
+def test_a_capture_on_a_stream_that_is_not_current_takes_a_workspace_of_its_own():
+    """A long window (parts in the workspace), captured through stream=: calls outside the graph may run beside its replays."""
+    w = make_window(1, 8, 2, 128, 64, 20000, seed=3)
+    fill_windows(w, [20000])
+    q = torch.randn((1, 8, 128), generator=torch.Generator(DEV).manual_seed(1), device=DEV).to(BF16)
+    side, out = torch.cuda.Stream(), torch.empty_like(q)
+    want = w.attend(q, stream=side)
+    torch.cuda.synchronize()
+    kept = {k: t.data_ptr() for k, t in w._ws.items()}
+    assert side.cuda_stream in kept
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin(capture_error_mode="thread_local")
+    w.attend(q, out=out, stream=side)
+    with torch.cuda.stream(side):
+        graph.capture_end()
+    assert {k: t.data_ptr() for k, t in w._ws.items()} == kept
+    out.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+
+
+def test_an_append_of_no_rows_changes_nothing():
+    w = make_window(2, 4, 2, 64, 16, 32, frequencies=pq.pq_rotary_frequencies(64))
+    w.lens.copy_(torch.tensor([3, 0], dtype=torch.int32))
+    pool = w.pool.clone()
+    q, k, v = (torch.empty((0, h, 64), dtype=BF16, device=DEV) for h in (4, 2, 2))
+    assert w.append(q, k, v, torch.zeros(3, dtype=torch.int32, device=DEV)).shape == q.shape
+    assert w.lens.cpu().tolist() == [3, 0] and torch.equal(w.pool, pool) and w.check_status()[0] == pq.OK
+
+
 def test_calls_on_two_streams_do_not_disturb_each_other():
     """Long windows of one sequence (parts in the workspace) attended on two streams at once."""
     w = make_window(1, 8, 2, 128, 64, 20000, seed=3)
