@@ -444,6 +444,8 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
 // tiles at least, more where a block still has 16 tiles for every stream (uneven lengths then level out), and a merge kernel (2.5 us) only
 // where a stream would have more than eight tiles.  us at 1, 2, 4, 8 splits, 32/8 heads: 16 sequences of 500 tokens 15.2, 13.7, 11.4, 16.8;
 // of 2048 43, 35, 27, 31; 64 of 200 16, 21, 29, 50; 64 of 1024 to 4096 129, 119, 111, 121; one of 4096 66, 35, 20, 12.4 and in eight parts 11.1.
+// Clusters of 3, 5, 6 and 7 where the wave stays a sixth below full: fuller ones no longer pack.  35 rows of eight sequences over 2048 tokens in
+// clusters of 4 and 5 23.2, 20.8; 20 sequences of 600 in 2 and 3 16.5, 15.0; 12 of 2048 in 4, 5 and 6 23.2, 22.2, 29.1; 10 of 1000 in 4, 6 and 7 15.4, 14.3, 19.5.
 struct WindowCut {
   int cluster, parts;
 };
@@ -454,6 +456,7 @@ static WindowCut cut_window(int64_t units, int max_len, int n_sm, int streams, i
   const int64_t splits = std::min(std::max<int64_t>(1, tiles / 2), std::max(one_wave, tiles / (16 * streams)));
   WindowCut c = {1, 1};
   while (c.cluster < kWinMaxCluster && 2 * c.cluster <= splits) c.cluster *= 2;
+  c.cluster = (int)std::max<int64_t>(c.cluster, std::min({splits, 10 * (int64_t)n_sm / (3 * units), (int64_t)kWinMaxCluster}));
   if (c.cluster == kWinMaxCluster)
     c.parts = (int)std::max<int64_t>(1, std::min({(tiles * steps + 64 * streams - 1) / (64 * streams), one_wave / kWinMaxCluster, (int64_t)kWinMaxParts}));
   return c;

@@ -306,7 +306,7 @@ static WindowRows window_rows_of_lanes(int d, int kv_dtype, int64_t all) {
   return window_rows_of(all == 1 ? 1 : all == 2 ? 2 : all <= 4 ? 4 : 8, kWinWarps, kv_dtype == PQ_DTYPE_F32 && d >= 64 ? d / 32 : 1, all);
 }
 // On tensor cores 16 rows and four streams are as fast as 64 and one (the blocks that share a window's tokens find them in L2), or faster where
-// that leaves no rows empty and needs no parts: 35 rows over 2048 tokens 23.0 and 24.5 us, 32 over 2000 15.3 and 17.3 (32 rows and two
+// that leaves no rows empty and needs no parts: 35 rows over 2048 tokens 23.0 and 24.5 us (clusters of four), 32 over 2000 15.3 and 17.3 (32 rows and two
 // streams), 64 over 4000 25.4 and 31.6, 64 over 2048 of 32 sequences 132 both.  With more than 48 rows over windows larger than L2 one
 // reading is: eight sequences of 8192 138 and 115.
 static WindowRows window_rows(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len) {

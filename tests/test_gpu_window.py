@@ -349,6 +349,20 @@ def test_large_scores_do_not_overflow():
     assert np.max(np.abs(f64(out[0]) - want[0])) < 0.3
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("B,hq,hkv", [(1, 3, 1), (70, 1, 1), (80, 2, 1), (45, 4, 2), (120, 1, 1), (150, 2, 1), (240, 1, 1), (500, 1, 1)])
+def test_clusters_of_every_size(B, hq, hkv, dtype):
+    """Batches that leave room for eight blocks a window, seven, six, ... one (on 148 SMs)."""
+    w = make_window(B, hq, hkv, 64, 16, 272, seed=B, dtype=dtype)
+    lens = [272 - (b * 37) % 130 if b % 9 else b % 3 for b in range(B)]
+    fill_windows(w, lens)
+    q = torch.randn((B, hq, 64), generator=torch.Generator(DEV).manual_seed(B), device=DEV).to(dtype)
+    lse = torch.empty((B, hq), dtype=torch.float32, device=DEV)
+    out = w.attend(q, lse=lse)
+    torch.cuda.synchronize()
+    check_attention(w, lens, q, out, lse, 64 ** -0.5)
+
+
 @pytest.mark.parametrize("max_len", [1, 128, 1024, 100000])
 def test_a_bound_on_the_lengths_changes_only_the_cut(max_len):
     lens = [900, 3]
