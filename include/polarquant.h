@@ -426,7 +426,9 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  * The angle is formed in float64 and reduced to a turn before its cosine and sine are taken in float32; products and sums are
  * float32, rounded once.  A sequence that would exceed pages_per_seq * page_tokens keeps its window and records
  * PQ_ERR_CAPACITY; a row whose page lies outside the pool is not written, its sequence does not grow, and PQ_ERR_INVALID_ARG
- * is recorded, as it is where cu[b+1] exceeds total_tokens.  The queries of such sequences are rotated all the same.
+ * is recorded, as it is where cu[b+1] exceeds total_tokens.  The queries of such sequences are rotated all the same.  Rows before
+ * cu[0] are no sequence's: they record PQ_ERR_INVALID_ARG.  Where cu falls anywhere, or starts below 0, no window grows, and an error
+ * is recorded.
  *
  * pq_window_attention: attention (Eq. 2) of the last n_q positions of every sequence over its window: query j sees the tokens
  * t < window_lens[b] - (n_q - 1 - j), as in pq_multi_query_attention.  Scores, softmax and sums are float32.

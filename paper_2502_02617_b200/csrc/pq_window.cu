@@ -1,6 +1,7 @@
 // The paged window of recent tokens: new rows on their way in, with the rotary position applied to queries and keys.  (The
 // attention that reads it is pq_window_attention.cuh.)
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "pq_common.cuh"
@@ -29,7 +30,11 @@ __device__ __forceinline__ bool append_fits(const AppendArgs& a, int base, int c
   return base >= 0 && (int64_t)base + count <= (int64_t)a.pg.page_tokens * a.pg.pages_per_seq;
 }
 __device__ __forceinline__ int64_t append_target(const AppendArgs& a, int seq, int base, int count, int place) {
-  if (!append_fits(a, base, count) || place < base || place - base >= count) {   // ends that do not rise leave rows before their sequence
+  if (place < base || place - base >= count) {   // a row before the first sequence's, or ends that fall: no sequence's
+    set_status(a.status, PQ_ERR_INVALID_ARG);
+    return -1;
+  }
+  if (!append_fits(a, base, count)) {
     set_status(a.status, PQ_ERR_CAPACITY);
     return -1;
   }
@@ -169,23 +174,42 @@ __global__ void __launch_bounds__(256) append_window_kernel(const __grid_constan
   }
 }
 
-// A sequence's window grows by its rows, all of them or, where one of them has no place, none.
-__device__ __forceinline__ void advance_window(const AppendArgs& a, int b) {
-  const int base = __ldcg(a.lens + b), count = a.cu_seqlens != nullptr ? __ldcg(a.cu_seqlens + b + 1) - __ldcg(a.cu_seqlens + b) : 1;
-  if (count <= 0 || !append_fits(a, base, count)) return;
-  if (a.cu_seqlens != nullptr && a.cu_seqlens[b + 1] > a.total_tokens) {   // rows that do not exist
+// Whether a sequence's row pointers fall, or lie below row 0.  The look-ups above take them to rise: where they do not, the rows of a sequence by
+// its own two ends are not the rows that were given to it, and a window that grew by them would hold rows nobody wrote.
+__device__ __forceinline__ bool ends_fall(int first, int end) { return first < 0 || end < first; }
+// A sequence's window grows by its rows, all of them or, where one of them has no place, none: its length after that, -1 where it stays.
+// `first`, `end`: its row pointers (0 and 1 where every sequence has one row).
+__device__ __forceinline__ int advanced_length(const AppendArgs& a, int b, int first, int end) {
+  const int base = __ldcg(a.lens + b), count = end - first;
+  if (count <= 0 || !append_fits(a, base, count)) return -1;
+  if (a.cu_seqlens != nullptr && end > a.total_tokens) {   // rows that do not exist
     set_status(a.status, PQ_ERR_INVALID_ARG);
-    return;
+    return -1;
   }
   for (int p = base / a.pg.page_tokens; p <= (base + count - 1) / a.pg.page_tokens; ++p)
-    if ((unsigned)__ldcg(a.pg.table + (int64_t)b * a.pg.pages_per_seq + p) >= (unsigned)a.pg.n_pages) return;
-  a.lens[b] = base + count;
+    if ((unsigned)__ldcg(a.pg.table + (int64_t)b * a.pg.pages_per_seq + p) >= (unsigned)a.pg.n_pages) return -1;
+  return base + count;
 }
 // A thread per sequence, behind a kernel that has every block say (launch_dependents) when it has read the lengths: the windows
 // grow while the rows are still on their way.  The wait at the end makes this kernel's end that of the rows' too.
 __global__ void __launch_bounds__(128) advance_windows_kernel(const __grid_constant__ AppendArgs a) {
   const int b = blockIdx.x * 128 + threadIdx.x;
-  if (b < a.batch) advance_window(a, b);
+  int first = 0, end = 1, length = -1;
+  bool falls = false;   // of any sequence: no window grows
+  if (b < a.batch) {
+    if (a.cu_seqlens != nullptr) {
+      first = __ldcg(a.cu_seqlens + b);
+      end = __ldcg(a.cu_seqlens + b + 1);
+    }
+    length = advanced_length(a, b, first, end);
+    falls = ends_fall(first, end);
+  }
+  if (a.cu_seqlens != nullptr)
+    for (int j = threadIdx.x; j < a.batch; j += 128)
+      if (j != b) falls = falls || ends_fall(__ldcg(a.cu_seqlens + j), __ldcg(a.cu_seqlens + j + 1));
+  falls = __syncthreads_or(falls);
+  if (length >= 0 && !falls) a.lens[b] = length;
+  if (falls && threadIdx.x == 0) set_status(a.status, PQ_ERR_INVALID_ARG);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 }
@@ -232,20 +256,34 @@ __global__ void __launch_bounds__(kApThreads) append_window_pieces_kernel(const 
     x[k] = ld_once(src);
     y[k] = ld_once(src + gap[k]);
   }
+  bool falls = false;
   if (a.cu_seqlens != nullptr) {   // the sequence of the block's first row: as many as end at it or before
     int seq = 0;
-    for (int j = 0; j < a.batch; j += kApThreads) seq += __syncthreads_count(j + tid < a.batch && a.cu_seqlens[j + tid + 1] <= token0);
+    for (int j = 0; j < a.batch; j += kApThreads) {
+      const bool is = j + tid < a.batch;
+      const int first = is ? a.cu_seqlens[j + tid] : 0, end = is ? a.cu_seqlens[j + tid + 1] : INT_MAX;
+      falls = falls || ends_fall(first, end);
+      seq += __syncthreads_count(end <= token0);
+    }
     if (tid < n_tokens) places[tid] = append_place(a, token0 + tid, seq);
   } else if (tid < n_tokens) {
     places[tid] = append_place(a, token0 + tid, token0 + tid);
   }
-  __syncthreads();
+  falls = __syncthreads_or(falls);
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // this block has read the lengths
   if (alone) {   // nobody else reads them
     if (a.cu_seqlens == nullptr) {
-      if (tid < n_tokens) advance_window(a, token0 + tid);
+      if (tid < n_tokens) {
+        const int length = advanced_length(a, token0 + tid, 0, 1);
+        if (length >= 0) a.lens[token0 + tid] = length;
+      }
+    } else if (falls) {
+      if (tid == 0) set_status(a.status, PQ_ERR_INVALID_ARG);
     } else {
-      for (int b = tid; b < a.batch; b += kApThreads) advance_window(a, b);
+      for (int b = tid; b < a.batch; b += kApThreads) {
+        const int length = advanced_length(a, b, __ldcg(a.cu_seqlens + b), __ldcg(a.cu_seqlens + b + 1));
+        if (length >= 0) a.lens[b] = length;
+      }
     }
   }
   for (int i = tid; i < n_tokens * a.half; i += kApThreads) {
