@@ -388,7 +388,11 @@ struct PrefixArgs {
     const pq_paging* pg = paging.get();
     const int64_t bytes = pg != nullptr ? pq_paged_cache_bytes(d, hkv, pg->page_tokens, pg->n_pages) : pq_cache_bytes(d, (int32_t)lens.size(0), hkv, capacity);
     check(bytes < 0 || (cache.is_contiguous() && (int64_t)cache.nbytes() >= bytes), "the cache is smaller than its sizes say");   // below 0: the call says why
-    if (pg != nullptr) check(tensor(PyTuple_GET_ITEM(a[13], 0)).size(0) == lens.size(0), "the page table must have a row for every length");
+    if (pg != nullptr) {
+      check(PyTuple_Check(a[13]), "paging is (page table, tokens per page, pages)");
+      const at::Tensor& table = tensor(PyTuple_GET_ITEM(a[13], 0));
+      check(table.size(0) == lens.size(0) && table.device() == cache.device(), "the page table must have a row for every length, on the cache's device");
+    }
   }
   int32_t queries() const { return (int32_t)(q.numel() / ((int64_t)d * hq)); }
 };
