@@ -586,7 +586,7 @@ __device__ __forceinline__ void combine_and_store(const DecodeArgs& a, int b, in
     if (lane == 0) {
       linv_sm[warp] = L > 0.f ? 1.f / L : 0.f;
       // scores are kept in the log2 domain: sum_t exp(s_t) = 2^M * L
-      if (a.lse != nullptr) a.lse[h0 + warp] = L > 0.f ? (M + log2f(L)) * 0.693147180559945309f : -CUDART_INF_F;
+      if (a.lse != nullptr) a.lse[h0 + warp] = L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f;   // NaN stays NaN
     }
   }
   __syncthreads();
@@ -1080,7 +1080,7 @@ __global__ void __launch_bounds__(kFastThreads, 1) decode_attention_fast_kernel(
       float M = ml.x;
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(half, M, o));
-      float l = ml.x == -CUDART_INF_F ? 0.f : ml.y * fast_exp2(ml.x - M);
+      float l = ml.y * (ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - M));   // 0 times a NaN stays one
 #pragma unroll
       for (int o = 8; o > 0; o >>= 1) l += __shfl_xor_sync(half, l, o);
       if ((tid & 15) == 0) __stcg(reinterpret_cast<float2*>(a.ws.ml) + (int64_t)slot * g_heads + h, make_float2(M, l));

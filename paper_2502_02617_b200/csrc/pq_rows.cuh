@@ -66,20 +66,20 @@ __device__ __forceinline__ void combine_rows(const DecodeArgs& a, const int2* in
     for (int s = l8; s < ns; s += 8) {
       const float2 ml = __ldcg(mlp + (int64_t)s * R);
       const float m_new = fmaxf(M, ml.x);
-      if (m_new > -CUDART_INF_F) L = L * fast_exp2(M - m_new) + ml.y * fast_exp2(ml.x - m_new);
+      L = m_new > -CUDART_INF_F ? L * fast_exp2(M - m_new) + ml.y * fast_exp2(ml.x - m_new) : L + ml.y;   // no reference yet: 0, or a NaN
       M = m_new;
     }
 #pragma unroll
     for (int o = 4; o > 0; o >>= 1) {
       const float m2 = __shfl_xor_sync(0xffffffffu, M, o), l2 = __shfl_xor_sync(0xffffffffu, L, o), m_new = fmaxf(M, m2);
-      if (m_new > -CUDART_INF_F) L = L * fast_exp2(M - m_new) + l2 * fast_exp2(m2 - m_new);
+      L = m_new > -CUDART_INF_F ? L * fast_exp2(M - m_new) + l2 * fast_exp2(m2 - m_new) : L + l2;
       M = m_new;
     }
     if (l8 == 0 && r < n_rows) {
       stat[2 * r] = M;
       stat[2 * r + 1] = L > 0.f ? 1.f / L : 0.f;
       if (a.lse != nullptr)   // scores are in the log2 domain
-        a.lse[info[r].x] = L > 0.f ? (M + log2f(L)) * 0.693147180559945309f : -CUDART_INF_F;
+        a.lse[info[r].x] = L == 0.f ? -CUDART_INF_F : (M + log2f(L)) * 0.693147180559945309f;   // NaN stays NaN
       else if (info[r].y <= 0) set_status(a.status, PQ_ERR_EMPTY);   // a query that sees no token
     }
   }
@@ -511,7 +511,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) rows_attention_kernel(DecodeAr
 #pragma unroll
         for (int w = 0; w < kRowWarps; ++w) {
           const float2 ml = *reinterpret_cast<const float2*>(mrg_ml + (w * kRowMax + tid) * 2);
-          l += ml.x == -CUDART_INF_F ? 0.f : ml.y * fast_exp2(ml.x - M);
+          l += ml.y * (ml.x == -CUDART_INF_F ? 0.f : fast_exp2(ml.x - M));   // 0 times a NaN stays one
         }
         __stcg(reinterpret_cast<float2*>(a.ws.ml) + (int64_t)slot * R + tid, make_float2(M, l));
       }

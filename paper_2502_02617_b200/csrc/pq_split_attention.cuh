@@ -374,7 +374,7 @@ __global__ void __launch_bounds__(32 * split_warps(kH), 1) split_attention_kerne
       float l = 0.f;
       if (lane < kSplitWarps) {
         const float m = wm_sm[lane * kH + h];
-        l = m == -CUDART_INF_F ? 0.f : wl_sm[lane * kH + h] * split_exp2(m - mb[h]);
+        l = wl_sm[lane * kH + h] * (m == -CUDART_INF_F ? 0.f : split_exp2(m - mb[h]));   // 0 times a NaN stays one
       }
 #pragma unroll
       for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
@@ -411,7 +411,11 @@ __global__ void __launch_bounds__(32 * split_warps(kH), 1) split_attention_kerne
       float m8 = M;
 #pragma unroll
       for (int r = 0; r < 8; ++r) m8 = fmaxf(m8, m[r]);
-      if (m8 == -CUDART_INF_F) continue;
+      if (m8 == -CUDART_INF_F) {   // no reference yet: denominators of 0, or of scores that are no numbers
+#pragma unroll
+        for (int r = 0; r < 8; ++r) L += l[r];
+        continue;
+      }
       const float k = split_exp2(M - m8);   // 0 at first
       L *= k;
       y.x *= k; y.y *= k; y.z *= k; y.w *= k;
