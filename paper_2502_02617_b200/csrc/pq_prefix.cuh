@@ -18,6 +18,12 @@
 namespace pq {
 
 constexpr int kPxThreads = 256, kPxWarps = kPxThreads / 32, kPxMaxParts = 32;
+// Weights are fp16 numbers 2^(s - reference), and a shared prefix is long: a reference at the largest score would leave all below 2^-25 of it at
+// 0, and 2^18 tokens at 2^-25.5 are half a percent of the sum.  It is kPxBelow under the largest score of its tile and moves when one is more
+// than kPxMost above it, so a weight is 2^15 at most and rounded by 2^-11 of itself or by 2^-32 of the largest one, whichever is more.
+// (prefix_mma_kernel's denominator sums the rounded weights, prefix_tc_kernel's the weights before that, which is 2.5 % faster there; the output
+// is off by those roundings, N 2^-32 for N small weights, either way.)
+constexpr float kPxBelow = 7.f, kPxMost = 15.f;
 template <int D, int kTiles>
 struct PxShape {
   static constexpr int kStreams = kPxWarps / kTiles, kRows = 16 * kTiles, kT = 16 * kTiles;   // tokens of a stream's tile
@@ -233,13 +239,14 @@ __global__ void __launch_bounds__(kPxThreads, kTiles <= 2 ? 2 : 1) prefix_mma_ke
     for (int n = 0; n < kN; ++n)
 #pragma unroll
       for (int h = 0; h < 2; ++h) mx[h] = fmaxf(mx[h], fmaxf(s[n][2 * h], s[n][2 * h + 1]));
-    const bool grow = mx[0] > m[0] + kLazyMax || mx[1] > m[1] + kLazyMax;   // true on the first tile (m is -inf), which has a token
-    if (__any_sync(0xffffffffu, grow)) {   // the reference moves only when a score is well above it (p <= 2^8 otherwise)
+    const bool grow = mx[0] > m[0] + kPxMost || mx[1] > m[1] + kPxMost;   // true on the first tile (m is -inf), which has a token
+    if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        float top = fmaxf(mx[h], m[h]);
+        float top = mx[h];
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        top = fmaxf(top - kPxBelow, m[h]);
         const float corr = win_rescale(m[h], top);
         m[h] = top;
         l[h] *= corr;

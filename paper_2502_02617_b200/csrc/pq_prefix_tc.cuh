@@ -169,10 +169,9 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
       // both halves' maxima are there, and both have read the scores whose columns P takes
       if (pc_owners_failed(fail)) break;
       mx = fmaxf(mx, row_max[((jb & 1) * 2 + (half ^ 1)) * 128 + row]);
-      // lazy reference: move it only when some score exceeds it by more than 8 (p <= 2^8 otherwise)
-      const bool grow = mx > m_run + 8.f || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);
+      const bool grow = mx > m_run + kPxMost || (m_run == -CUDART_INF_F && mx > -CUDART_INF_F);   // lazy reference: see kPxBelow
       if (__any_sync(0xffffffffu, grow)) {
-        const float m_new = grow ? mx : m_run;
+        const float m_new = grow ? mx - kPxBelow : m_run;
         const float corr = m_run == -CUDART_INF_F ? 1.f : fast_exp2(m_run - m_new);   // nothing accumulated yet: nothing to scale
         if (jb > 0) {
           // the value MMAs up to block jb - 1 must have completed before the accumulator is touched
@@ -204,7 +203,7 @@ __global__ void __launch_bounds__(kPcThreads, 1) prefix_tc_kernel(DecodeArgs a) 
         x0 = fast_exp2(x0);
         x1 = fast_exp2(x1);
         pw[e] = as_u32(__floats2half2_rn(x0, x1));
-        // the denominator before the rounding to fp16, which is as often up as down: its sum is off by 2^-12 of a weight's share
+        // the denominator, before the rounding to fp16: see kPxBelow
         pt_add2(sum4[2 * (e & 1)], sum4[2 * (e & 1) + 1], x0, x1, sum4[2 * (e & 1)], sum4[2 * (e & 1) + 1]);
       }
       tc_st16u_nowait(trow + kPtTmS + 64 * t + 16 * half, pw);
