@@ -438,7 +438,8 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  *                      zeros; without lse_dev the former records PQ_ERR_EMPTY, with it lse = -inf says so
  *   workspace_dev      pq_window_workspace_bytes(...) bytes; need not be initialised; two calls that overlap in time must not
  *                      share it
- * head_dim is 16, 32, 64 or 128 (of the window), batch at most 65535.  What rows past a window's end hold does not matter.
+ * head_dim is 16, 32, 64 or 128 (of the window), batch and n_kv_heads at most 65535, n_q * n_q_heads / n_kv_heads at most 2^24.
+ * What rows past a window's end hold does not matter.
  */
 int32_t pq_rotary_frequencies(int32_t rotary_dim, double theta, double* frequencies_host);
 int64_t pq_window_bytes(int32_t head_dim, int32_t n_kv_heads, int32_t page_tokens, int32_t n_pages, int32_t dtype);

@@ -1000,7 +1000,6 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     const int n_sm = pq::sm_count_of_device(sm_count);
     if (n_sm == 0) return PQ_ERR_CUDA;
     const pq::PrefixCut cut = pq::cut_prefix(n_q, n_kv_heads, g, max_len, std::min(n_sm, pq::kFastMaxGridHost));
-    if ((int64_t)n_kv_heads * cut.row_blocks > 65535) return PQ_ERR_UNSUPPORTED;
     switch (head_dim) {
       case 16: return pq::launch_prefix<16>(a, *shared, workspace_dev, cut, st);
       case 32: return pq::launch_prefix<32>(a, *shared, workspace_dev, cut, st);
@@ -1278,6 +1277,8 @@ int32_t pq_dequant_kv_paged(int32_t head_dim, int32_t n_kv_heads, const float* S
                        n_tokens, x_hat_dev, stream);
 }
 
+// (query, head) rows of a kv head of one sequence: 2^21 blocks of 8 rows and 2^7 splits of their tokens stay below 2^31 blocks.
+static constexpr int64_t kWindowMostRows = 1 << 24;
 
 int64_t pq_window_workspace_bytes(int32_t head_dim, int32_t batch, int32_t n_q, int32_t n_q_heads, int32_t n_kv_heads, int32_t max_len) {
   if (!pq::window_head_dim(head_dim)) return PQ_ERR_UNSUPPORTED;
@@ -1303,7 +1304,7 @@ static int32_t window_call(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_hea
   if (((uintptr_t)window_lens_dev | (uintptr_t)lse_dev | (uintptr_t)status_dev) & 3) return PQ_ERR_ALIGNMENT;
   const int g = n_q_heads / n_kv_heads;
   const pq::WindowRows rows = pq::window_rows(head_dim, kv_dtype, batch, n_q, n_kv_heads, g, max_len);
-  if (batch > 65535 || n_kv_heads * rows.blocks > 65535) return PQ_ERR_UNSUPPORTED;
+  if (batch > 65535 || n_kv_heads > 65535 || (int64_t)n_q * g > kWindowMostRows) return PQ_ERR_UNSUPPORTED;
   call->kv_dtype = kv_dtype; call->rows = rows; call->batch = batch; call->max_len = max_len;
   a.d = head_dim; a.n_q_heads = n_q_heads; a.n_kv_heads = n_kv_heads; a.n_q = n_q; a.io_dtype = io_dtype; a.out_dtype = out_dtype; a.early = 0;
   a.row_blocks = (int)rows.blocks; a.n_parts = 1; a.n_rows = (int64_t)batch * n_q * n_q_heads; a.scale = scale;

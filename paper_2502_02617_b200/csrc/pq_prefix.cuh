@@ -35,7 +35,7 @@ struct PxShape {
 };
 
 struct PrefixKernelArgs {
-  int n_q_heads, n_kv_heads, n_queries, row_blocks;
+  int n_q_heads, n_kv_heads, n_queries, n_splits;   // n_splits: see WindowArgs
   int64_t n_rows;
   const Tables* tables;
   const uint8_t* cache;
@@ -126,15 +126,15 @@ __global__ void __launch_bounds__(kPxThreads, kTiles <= 2 ? 2 : 1) prefix_mma_ke
   extern __shared__ __align__(128) uint8_t px_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, c4 = lane & 3;
   const int stream = warp / kTiles, tile = warp % kTiles;
-  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks;
+  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y, n_splits = a.n_splits, rb = blockIdx.x / n_splits, split = blockIdx.x % n_splits;
   const int r0 = rb * W::kRows, n_rows = min(W::kRows, a.n_queries * g - r0);   // row r0 + r: query (r0 + r) / g, head hk * g + (r0 + r) % g
   const uint32_t sm = (uint32_t)__cvta_generic_to_shared(px_smem);
   if (tid < PQ_N_CENTROIDS) reinterpret_cast<float2*>(px_smem + W::kTab)[tid] = make_float2(a.tables->cen_cos[tid], a.tables->cen_sin[tid]);   // a constant
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");   // behind the wait: see WindowArgs::early
   const int len = max(*a.len, 0);
-  const int tiles_all = (len + kT - 1) / kT, n_splits = gridDim.x;
-  const int first = (int)((int64_t)tiles_all * blockIdx.x / n_splits), n_tiles = (int)((int64_t)tiles_all * (blockIdx.x + 1) / n_splits) - first;
+  const int tiles_all = (len + kT - 1) / kT;
+  const int first = (int)((int64_t)tiles_all * split / n_splits), n_tiles = (int)((int64_t)tiles_all * (split + 1) / n_splits) - first;
   const int mine = n_tiles > stream ? (n_tiles - stream + W::kStreams - 1) / W::kStreams : 0;
   auto row_of = [&](int r) -> int64_t {
     const int j = (r0 + r) / g;
@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kPxThreads, kTiles <= 2 ? 2 : 1) prefix_mma_ke
   merge_streams<D, kPxThreads, W::kStreams, W::kRows>(o_sm, ml_sm, n_rows);
   uint32_t n_blocks;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
-  const int64_t part = blockIdx.x / n_blocks;
+  const int64_t part = split / n_blocks;
   cluster_merge<D, kPxThreads>(o_sm, ml_sm, n_rows, [&](int r, int c, const float4& acc, float lse) {
     const int64_t row = row_of(r);
     *reinterpret_cast<float4*>(a.part_out + (part * a.n_rows + row) * D + c) = acc;
@@ -567,7 +567,7 @@ static int32_t launch_prefix_mma(const PrefixKernelArgs& a, const PrefixCut& cut
   static DeviceMemo configured;
   if (configure_for_device(prefix_mma_kernel<D, kTiles>, PxShape<D, kTiles>::kBytes, configured) == 0) return PQ_ERR_CUDA;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cut.cluster * cut.parts, a.n_kv_heads * cut.row_blocks);
+  cfg.gridDim = dim3((unsigned)a.n_splits * cut.row_blocks, a.n_kv_heads);
   cfg.blockDim = dim3(kPxThreads);
   cfg.dynamicSmemBytes = PxShape<D, kTiles>::kBytes;
   cfg.stream = stream;
@@ -612,7 +612,7 @@ static int32_t finish_prefix(const DecodeArgs& d, const SharedPrefix& shared, co
 template <int D>
 static int32_t launch_prefix(const DecodeArgs& d, const SharedPrefix& shared, void* workspace, const PrefixCut& cut, cudaStream_t stream) {
   PrefixKernelArgs a;
-  a.n_q_heads = d.n_q_heads; a.n_kv_heads = d.n_kv_heads; a.n_queries = d.n_q; a.row_blocks = cut.row_blocks;
+  a.n_q_heads = d.n_q_heads; a.n_kv_heads = d.n_kv_heads; a.n_queries = d.n_q; a.n_splits = cut.cluster * cut.parts;
   a.n_rows = (int64_t)d.n_q * d.n_q_heads;
   a.tables = d.tables; a.cache = d.cache; a.len = d.lens; a.status = d.status; a.pg = d.pg;
   __half* qrot = reinterpret_cast<__half*>(workspace);

@@ -20,6 +20,8 @@ constexpr int kWinThreads = 128, kWinWarps = kWinThreads / 32, kWinMaxCluster = 
 
 struct WindowArgs {
   int d, n_q_heads, n_kv_heads, n_q, io_dtype, out_dtype, row_blocks, n_parts;
+  int n_splits;         // blocks that share a row block's tokens.  A row block's follow one another in the grid's first dimension, and so do the row
+                        // blocks: the other dimensions end at 65535 (16384 positions of 64/8 heads are 65536 blocks of 16 rows)
   int early;            // the kernel ahead in the stream writes nothing that this one reads, and has every block say (launch_dependents)
                         // when all before it is done: wait for it at the end only, and use the SMs that it leaves idle
   int64_t n_rows;       // batch * n_q * n_q_heads: rows of q, out and of a part
@@ -158,7 +160,7 @@ template <int D, class RowOf, class Seen>
 __device__ __forceinline__ void window_finish(const WindowArgs& a, const float* y, const float2* bl, int n_rows, RowOf row_of, Seen seen) {
   uint32_t n_blocks;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n_blocks));
-  const int part = blockIdx.x / n_blocks;
+  const int part = blockIdx.x % a.n_splits / n_blocks;
   cluster_merge<D, kWinThreads>(y, bl, n_rows, [&](int r, int c, const float4& acc, float lse) {
     const int64_t row = row_of(r), at = row * D + c;
     if (a.n_parts > 1) {
@@ -213,7 +215,7 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
   __shared__ __align__(16) float y_sm[kRows][D];            // the block's merged output, read by the cluster
   __shared__ float2 ml_sm[kWinWarps][kRows], bl_sm[kRows];  // (reference, denominator) of the warps and of the block
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, li = lane & (kLanes - 1), group = lane / kLanes;
-  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks, b = blockIdx.z;
+  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y, n_splits = a.n_splits, rb = blockIdx.x / n_splits, split = blockIdx.x % n_splits, b = blockIdx.z;
   const int r0 = rb * kRows, n_rows = min(kRows, a.n_q * g - r0);   // row r0 + r: query (r0 + r) / g, head hk * g + (r0 + r) % g
   window_begin(a);
   auto row_of = [&](int r) -> int64_t {   // of q, out and lse
@@ -224,9 +226,9 @@ __global__ void __launch_bounds__(kWinThreads) window_attention_kernel(const __g
   auto seen = [&](int r) { return max(0, len - (a.n_q - 1 - (r0 + r) / g)); };
   const int most = seen(n_rows - 1), least = seen(0);
   // this block's range of the tokens: whole pieces of 16
-  const int pieces = (most + 15) / 16, n_splits = gridDim.x;
-  const int t_begin = (int)((int64_t)pieces * blockIdx.x / n_splits) * 16;
-  const int t_end = min(most, (int)((int64_t)pieces * (blockIdx.x + 1) / n_splits) * 16);
+  const int pieces = (most + 15) / 16;
+  const int t_begin = (int)((int64_t)pieces * split / n_splits) * 16;
+  const int t_end = min(most, (int)((int64_t)pieces * (split + 1) / n_splits) * 16);
 
   uint64_t q[kRows][kP], o[kRows][kP];
 #pragma unroll
@@ -464,7 +466,7 @@ static WindowCut cut_window(int64_t units, int max_len, int n_sm, int streams, i
 
 static int32_t launch_window(void (*kernel)(WindowArgs), const WindowArgs& a, int batch, const WindowCut& cut, int smem, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(cut.cluster * cut.parts, a.n_kv_heads * a.row_blocks, batch);
+  cfg.gridDim = dim3((unsigned)a.n_splits * a.row_blocks, a.n_kv_heads, batch);
   cfg.blockDim = dim3(kWinThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;

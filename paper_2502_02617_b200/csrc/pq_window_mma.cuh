@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid
   extern __shared__ __align__(128) uint8_t wm_smem[];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g8 = lane >> 2, c4 = lane & 3;
   const int stream = warp / kTiles, tile = warp % kTiles, in_stream = tid % kThreads;
-  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y / a.row_blocks, rb = blockIdx.y % a.row_blocks, b = blockIdx.z;
+  const int g = a.n_q_heads / a.n_kv_heads, hk = blockIdx.y, n_splits = a.n_splits, rb = blockIdx.x / n_splits, split = blockIdx.x % n_splits, b = blockIdx.z;
   const int r0 = rb * W::kRows, n_rows = min(W::kRows, a.n_q * g - r0);   // row r0 + r: query (r0 + r) / g, head hk * g + (r0 + r) % g
   const uint32_t sm = (uint32_t)__cvta_generic_to_shared(wm_smem);
   window_begin(a);
@@ -84,9 +84,9 @@ __global__ void __launch_bounds__(kWinThreads, 4) window_mma_kernel(const __grid
   const int len = min(max(__ldcg(a.lens + b), 0), P * a.pg.pages_per_seq);
   auto seen = [&](int r) { return max(0, len - (a.n_q - 1 - (r0 + r) / g)); };
   const int most = seen(n_rows - 1), least = seen(0);
-  const int pieces = (most + 15) / 16, n_splits = gridDim.x;
-  const int t_begin = (int)((int64_t)pieces * blockIdx.x / n_splits) * 16;
-  const int t_end = min(most, (int)((int64_t)pieces * (blockIdx.x + 1) / n_splits) * 16);
+  const int pieces = (most + 15) / 16;
+  const int t_begin = (int)((int64_t)pieces * split / n_splits) * 16;
+  const int t_end = min(most, (int)((int64_t)pieces * (split + 1) / n_splits) * 16);
   const int n_tiles = (t_end - t_begin + kWmTile - 1) / kWmTile;
   const int mine = n_tiles > stream ? (n_tiles - stream + W::kStreams - 1) / W::kStreams : 0;   // tiles of this stream
 
@@ -355,6 +355,7 @@ static int32_t launch_window_call(const WindowCall& w, bool early, cudaStream_t 
                                    w.rows.steps);
   a.early = early;
   a.n_parts = cut.parts;
+  a.n_splits = cut.cluster * cut.parts;
   a.part_lse = a.part_out + (cut.parts > 1 ? cut.parts * a.n_rows * a.d : 0);
   const int32_t st = launch_window_attention(a, w.kv_dtype, w.rows.rows, w.batch, cut, stream);
   if (st != PQ_OK || cut.parts == 1) return st;
