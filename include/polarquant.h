@@ -402,8 +402,9 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  *
  * The pool: [n_pages][n_kv_heads][K | V][page_tokens][head_dim] elements of one dtype (pq_window_bytes), contiguous, so the
  * rows of a page can be read as they are (e.g. to be encoded into the packed cache later).  pq_paging as above, but
- * page_tokens is any multiple of 16; token w of sequence b's window is row w % page_tokens of physical page
- * page_table[b * pages_per_seq + w / page_tokens].  window_lens_dev, int32[batch]: tokens in each window.
+ * page_tokens is any multiple of 16, pages_per_seq * page_tokens at most 2^31 - 256; token w of sequence b's window is row
+ * w % page_tokens of physical page page_table[b * pages_per_seq + w / page_tokens].  window_lens_dev, int32[batch]: tokens in
+ * each window.
  *
  * pq_rotary_frequencies (host): frequencies_host[i] = theta^(-2 i / rotary_dim), i < rotary_dim / 2 (rotary_dim even).  Any
  * other frequencies (scaled ones, say) can be used in their place.

@@ -15,7 +15,8 @@ inline bool window_head_dim(int d) { return d == 16 || d == 32 || d == 64 || d =
 inline int32_t window_paging_from(const pq_paging* p, Paging* out) {
   if (p == nullptr || p->page_table_dev == nullptr) return PQ_ERR_INVALID_ARG;
   if (p->page_tokens <= 0 || p->page_tokens % 16 || p->pages_per_seq <= 0 || p->n_pages <= 0) return PQ_ERR_INVALID_ARG;
-  if ((int64_t)p->page_tokens * p->pages_per_seq >= (1ll << 31)) return PQ_ERR_UNSUPPORTED;
+  // a warp's next step, up to 64 tokens behind the last one it reads, is a position in 32 bits too
+  if ((int64_t)p->page_tokens * p->pages_per_seq > (1ll << 31) - 256) return PQ_ERR_UNSUPPORTED;
   if ((uintptr_t)p->page_table_dev & 3) return PQ_ERR_ALIGNMENT;
   out->table = p->page_table_dev; out->page_tokens = p->page_tokens; out->pages_per_seq = p->pages_per_seq;
   out->n_pages = p->n_pages;
