@@ -89,7 +89,7 @@ __device__ __forceinline__ uint32_t pair_bf16(float a, float b) {
   const __nv_bfloat162 w = __floats2bfloat162_rn(a, b);
   return *reinterpret_cast<const uint32_t*>(&w);
 }
-// Elements e of x and of y are a pair, with the cosine and sine c[e].
+// Elements e of x and of y are a pair, with the cosine and sine c[e] (bf16: c on 16 bytes).
 template <class T>
 __device__ __forceinline__ void turn_halves(uint4& x, uint4& y, const float2* c) {
   uint32_t a[4] = {x.x, x.y, x.z, x.w}, b[4] = {y.x, y.y, y.z, y.w};
@@ -224,7 +224,8 @@ template <class T>
 __global__ void __launch_bounds__(kApThreads) append_window_pieces_kernel(const __grid_constant__ AppendArgs a, int tokens, int slices,
                                                                           bool alone) {
   constexpr int kV = 16 / sizeof(T);
-  __shared__ float2 cs[kApTokens][kApMaxHalf];
+  static_assert(kApMaxHalf * sizeof(float2) % 16 == 0, "turn_halves reads two pairs of a row at a time");
+  __shared__ __align__(16) float2 cs[kApTokens][kApMaxHalf];
   __shared__ AppendPlace places[kApTokens];
   const int tid = threadIdx.x, token0 = blockIdx.x / slices * tokens, slice = blockIdx.x % slices;
   const int n_tokens = min(tokens, a.total_tokens - token0);
