@@ -307,8 +307,9 @@ __global__ void __launch_bounds__(kPxThreads, kTiles <= 2 ? 2 : 1) prefix_mma_ke
 
 // ---- the rotations before and after, on tensor cores (mma.sync)
 // A block of eight warps takes 16 rows (32 and 64 at head_dim 32 and 16); a warp has kNt columns of eight.  S is copied to shared memory
-// before the kernel ahead in the stream has finished; its elements and float32 rows are two bf16 terms each (16 bits: an error of
-// 2^-16 in a rotated coordinate, where the products with the decoded keys carry 2^-11), bf16 queries are one; small products first.
+// before the kernel ahead in the stream has finished.  Before the attention its elements and float32 queries are three bf16 terms each (24 bits,
+// so that the scores keep the 22 of the rotated queries and keys; two moved the log-sum-exp of scores of a few hundred by twice as much as the
+// rest), bf16 queries are one.  After it two of each are enough: an error of 2^-16 on outputs whose values carry 2^-12.  Small products first.
 template <int D>
 struct PrShape {
   static constexpr int kNt = D == 128 ? 2 : 1, kTileWarps = D / 8 / kNt, kTiles = 8 / kTileWarps, kRows = 16 * kTiles, kSteps = D / 16;
@@ -316,9 +317,10 @@ struct PrShape {
   static constexpr int kBytes = (D * kStride + kRows * kXStride + kRows) * 4;
 };
 constexpr int kPrThreads = 256;
-__device__ __forceinline__ void bf16_two_terms(float a, float b, uint32_t* t) {
+template <int kTerms>
+__device__ __forceinline__ void pr_terms(float a, float b, uint32_t* t) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < kTerms; ++i) {
     const __nv_bfloat162 w = __floats2bfloat162_rn(a, b);
     t[i] = *reinterpret_cast<const uint32_t*>(&w);
     a -= __uint_as_float(t[i] << 16);
@@ -331,22 +333,24 @@ __device__ __forceinline__ void pr_stage(const float* S, float* s) {
   for (int i = threadIdx.x; i < D * D / 4; i += kPrThreads)
     *reinterpret_cast<float4*>(s + i / (D / 4) * PrShape<D>::kStride + 4 * (i % (D / 4))) = __ldg(reinterpret_cast<const float4*>(S) + i);
 }
-// d += a times columns n .. n + 7 of S (kTransposed: of S^T) at k-step ks; kTerms: of a.
-template <int D, bool kTransposed, int kTerms>
-__device__ __forceinline__ void pr_mma(float* d, const uint32_t (&a)[2][4], const float* s, int ks, int n, int g8, int c4) {
+// d += a times columns n .. n + 7 of S (kTransposed: of S^T) at k-step ks; kTerms: of a, kOfS: of S.
+template <int D, bool kTransposed, int kTerms, int kOfS>
+__device__ __forceinline__ void pr_mma(float* d, const uint32_t (&a)[kTerms][4], const float* s, int ks, int n, int g8, int c4) {
   constexpr int kStride = PrShape<D>::kStride;
-  uint32_t f[2][2];
+  uint32_t f[2][kOfS];
 #pragma unroll
   for (int e = 0; e < 2; ++e) {   // rows 2 c4, + 1 of the step's first or second eight, column n + g8
     const int k = 16 * ks + 8 * e + 2 * c4;
     float2 v;
     if constexpr (kTransposed) v = *reinterpret_cast<const float2*>(s + (n + g8) * kStride + k);
     else v = make_float2(s[k * kStride + n + g8], s[(k + 1) * kStride + n + g8]);
-    bf16_two_terms(v.x, v.y, f[e]);
+    pr_terms<kOfS>(v.x, v.y, f[e]);
   }
-  if constexpr (kTerms == 2) mma_bf16_16816(d, a[1], f[0][0], f[1][0]);
-  mma_bf16_16816(d, a[0], f[0][1], f[1][1]);
-  mma_bf16_16816(d, a[0], f[0][0], f[1][0]);
+#pragma unroll
+  for (int order = kOfS - 1; order >= 0; --order)   // products below 2^(-8 kOfS) are left out
+#pragma unroll
+    for (int i = kTerms - 1; i >= 0; --i)
+      if (i <= order) mma_bf16_16816(d, a[i], f[0][order - i], f[1][order - i]);
 }
 
 // q' = (q S) * factor of every row as fp16 value and residual: qrot [row][value | residual][D], coordinate j at (j & ~3) | (0, 2, 1, 3)[j & 3].
@@ -361,7 +365,8 @@ __global__ void __launch_bounds__(kPrThreads) prefix_rotate_kernel(const float* 
   pr_stage<D>(S, pr_smem);   // a constant of the caller
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int64_t at[2] = {min(row0 + g8, n_rows - 1) * D + 2 * c4, min(row0 + g8 + 8, n_rows - 1) * D + 2 * c4};   // rows past the last repeat it
-  uint32_t a[W::kSteps][2][4];
+  constexpr int kTerms = kBf16 ? 1 : 3;
+  uint32_t a[W::kSteps][kTerms][4];
 #pragma unroll
   for (int ks = 0; ks < W::kSteps; ++ks)
 #pragma unroll
@@ -371,10 +376,10 @@ __global__ void __launch_bounds__(kPrThreads) prefix_rotate_kernel(const float* 
         a[ks][0][i] = *reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(q) + k);
       } else {
         const float2 v = *reinterpret_cast<const float2*>(reinterpret_cast<const float*>(q) + k);
-        uint32_t w[2];
-        bf16_two_terms(v.x, v.y, w);
-        a[ks][0][i] = w[0];
-        a[ks][1][i] = w[1];
+        uint32_t w[kTerms];
+        pr_terms<kTerms>(v.x, v.y, w);
+#pragma unroll
+        for (int e = 0; e < kTerms; ++e) a[ks][e][i] = w[e];
       }
     }
   __syncthreads();
@@ -384,7 +389,7 @@ __global__ void __launch_bounds__(kPrThreads) prefix_rotate_kernel(const float* 
 #pragma unroll
   for (int ks = 0; ks < W::kSteps; ++ks)
 #pragma unroll
-    for (int t = 0; t < W::kNt; ++t) pr_mma<D, false, kBf16 ? 1 : 2>(acc[t], a[ks], pr_smem, ks, n0 + 8 * t, g8, c4);
+    for (int t = 0; t < W::kNt; ++t) pr_mma<D, false, kTerms, 3>(acc[t], a[ks], pr_smem, ks, n0 + 8 * t, g8, c4);
 #pragma unroll
   for (int t = 0; t < W::kNt; ++t)
 #pragma unroll
@@ -497,12 +502,12 @@ __global__ void __launch_bounds__(kPrThreads) prefix_unrotate_kernel(const float
     for (int i = 0; i < 4; ++i) {
       const float2 v = *reinterpret_cast<const float2*>(x + (16 * tile + g8 + 8 * (i & 1)) * W::kXStride + 16 * ks + 2 * c4 + 8 * (i >> 1));
       uint32_t w[2];
-      bf16_two_terms(v.x, v.y, w);
+      pr_terms<2>(v.x, v.y, w);
       a[0][i] = w[0];
       a[1][i] = w[1];
     }
 #pragma unroll
-    for (int t = 0; t < W::kNt; ++t) pr_mma<D, true, 2>(y[t], a, pr_smem, ks, n0 + 8 * t, g8, c4);
+    for (int t = 0; t < W::kNt; ++t) pr_mma<D, true, 2, 2>(y[t], a, pr_smem, ks, n0 + 8 * t, g8, c4);
   }
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
