@@ -196,24 +196,32 @@ def _new_like(q, stream, device):
         return torch.empty_like(q, memory_format=torch.contiguous_format)
 
 
-def _stream_workspace(kept: dict, need: int, stream, device):
-    """At least `need` bytes that belong to `stream` (None: the device's current one): calls on different streams may overlap, so each
-    has its own.  A capture takes a new one from the graph's pool every time: calls outside must not share it with a replay."""
+def _take_workspace(kept: dict, need: int, stream, device):
+    """(key, workspace of at least `need` bytes that belongs to `stream`, None: the device's current one) for one call, which gives it back with
+    _keep_workspace: calls on different streams may overlap, and so may the launches of calls of several threads on one stream, so each has its
+    own.  A capture takes a new one from the graph's pool every time, which is not kept: calls outside must not share it with a replay."""
     key = (_native or native()).current_stream(device.index) if stream is None else stream.cuda_stream
-    ws = kept.get(key)
     if stream is None:
         capturing = torch.cuda.is_current_stream_capturing()
     else:
         with _on(stream, device):   # whichever is current outside
             capturing = torch.cuda.is_current_stream_capturing()
-    if ws is None or ws.numel() < need or capturing:
+    ws = None if capturing else kept.pop(key, None)
+    if ws is None or ws.numel() < need:
         with _on(stream, device):
             ws = torch.empty(need, dtype=torch.uint8, device=device)
-        if not capturing:
-            while len(kept) >= 8 and key not in kept:   # of streams that are no longer used
-                kept.pop(next(iter(kept)))
-            kept[key] = ws
-    return ws
+    return None if capturing else key, ws
+
+
+def _keep_workspace(kept: dict, key, ws):
+    if key is None:
+        return
+    while len(kept) >= 8:   # of streams that are no longer used
+        try:
+            kept.pop(next(iter(kept)), None)
+        except (RuntimeError, StopIteration):   # another thread was there
+            pass
+    kept[key] = ws
 
 
 def _dtype_code(t: torch.Tensor) -> int:
@@ -576,13 +584,15 @@ class PolarQuantCache:
 
     def _shared_workspace(self, stream, size, *args):
         if self._shared_ws is None:
-            self._shared_ws, self._shared_need = {}, {}
+            self._shared_ws = {}
+        if self._shared_need is None:
+            self._shared_need = {}
         need = self._shared_need.get(args)
         if need is None:
             if len(self._shared_need) >= 1024:   # of bounds that change with every call
                 self._shared_need.clear()
             need = self._shared_need[args] = size(self.d, *args)
-        return _stream_workspace(self._shared_ws, need, stream, self.cache.device)
+        return _take_workspace(self._shared_ws, need, stream, self.cache.device)
 
     def attend_prefix(self, q, seq=0, out=None, scale=None, max_len=None, lse=None, stream=None):
         """q [B, Hq, d] or [B, n_q, Hq, d] of any batch: every query attends to all tokens of sequence `seq` of this cache, which
@@ -590,9 +600,10 @@ class PolarQuantCache:
         if out is None:
             out = _new_like(q, stream, self.device)
         most = self.capacity if max_len is None else max_len
-        ws = self._shared_workspace(stream, pq_prefix_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
+        key, ws = self._shared_workspace(stream, pq_prefix_workspace_bytes, q.numel() // (q.shape[-1] * q.shape[-2]), q.shape[-2], self.n_kv_heads, most)
         pq_prefix_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
                             self.d ** -0.5 if scale is None else scale, out, lse, ws, self.status, self._paging_args(), stream)
+        _keep_workspace(self._shared_ws, key, ws)
         return out
 
     def attend_shared(self, q, window, seq=0, out=None, scale=None, max_len=None, max_window=None, stream=None):
@@ -601,11 +612,12 @@ class PolarQuantCache:
         if out is None:
             out = _new_like(q, stream, self.device)
         most, most_window = self.capacity if max_len is None else max_len, window.capacity if max_window is None else max_window
-        ws = self._shared_workspace(stream, pq_shared_workspace_bytes, q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2], self.n_kv_heads,
-                                    most, most_window)
+        key, ws = self._shared_workspace(stream, pq_shared_workspace_bytes, q.shape[0], q.shape[1] if q.dim() == 4 else 1, q.shape[-2], self.n_kv_heads,
+                                         most, most_window)
         pq_shared_attention(self.S, self.tables, q, self.cache, self.lens, seq, self.n_kv_heads, self.capacity, most,
                             self.d ** -0.5 if scale is None else scale, out, ws, self.status, window.pool, window.lens, most_window,
                             window._paging_args(), self._paging_args(), stream)
+        _keep_workspace(self._shared_ws, key, ws)
         return out
 
     def unpack(self, n_tokens):
@@ -733,8 +745,8 @@ class PagedWindow:
                 self._need.clear()
             need = self._need[n_q, max_len] = pq_window_workspace_bytes(self.d, self.batch, n_q, self.n_q_heads, self.n_kv_heads, max_len)
         if need <= self._unused.numel():   # one part: nothing is written
-            return self._unused
-        return _stream_workspace(self._ws, need, stream, self.device)
+            return None, self._unused
+        return _take_workspace(self._ws, need, stream, self.device)
 
     def attend(self, q, out=None, scale=None, max_len=None, lse=None, stream=None):
         """q [B, Hq, d], or [B, n_q, Hq, d] for the last n_q positions of every window (causal).  max_len: a bound on the lengths.
@@ -742,8 +754,10 @@ class PagedWindow:
         if out is None:
             out = _new_like(q, stream, self.device)
         most = self.capacity if max_len is None else max_len
-        pq_window_attention(q, self.pool, self.lens, most, self.d ** -0.5 if scale is None else scale, out, lse,
-                            self._workspace(q.shape[1] if q.dim() == 4 else 1, most, stream), self.status, self._paging_args(), stream)
+        key, ws = self._workspace(q.shape[1] if q.dim() == 4 else 1, most, stream)
+        pq_window_attention(q, self.pool, self.lens, most, self.d ** -0.5 if scale is None else scale, out, lse, ws, self.status, self._paging_args(),
+                            stream)
+        _keep_workspace(self._ws, key, ws)
         return out
 
     def check_status(self):
