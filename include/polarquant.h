@@ -432,7 +432,8 @@ int32_t pq_tail_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_head
  * is recorded.
  *
  * pq_window_attention: attention (Eq. 2) of the last n_q positions of every sequence over its window: query j sees the tokens
- * t < window_lens[b] - (n_q - 1 - j), as in pq_multi_query_attention.  Scores, softmax and sums are float32.
+ * t < window_lens[b] - (n_q - 1 - j), as in pq_multi_query_attention.  Scores, softmax and sums are float32; over a bf16 window
+ * of head_dim 64 or 128 the softmax's weights meet the values as two bf16 terms (17 bits).
  *   q_dev, out_dev     [batch][n_q][n_q_heads][head_dim] of io_dtype; kv_dtype: the pool's (either of the two)
  *   max_len            host-side upper bound on window_lens[b] (used only to cut the work)
  *   lse_dev            float32 [batch][n_q][n_q_heads] or NULL.  A query that sees no token, or only scores of -inf, yields
@@ -470,7 +471,8 @@ int32_t pq_window_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_kv_he
  *   max_len           host-side upper bound on that length
  *   lse_dev           float32 [n_queries][n_q_heads] or NULL; with it an empty prefix yields zeros and -inf and is no error
  *   workspace_dev     pq_prefix_workspace_bytes(...) bytes; as for pq_decode_attention
- * Tolerances are those of pq_multi_query_attention.
+ * Tolerances are those of pq_multi_query_attention: scores keep 22 bits of keys and rotated queries, values and the softmax's
+ * weights are fp16 in their product, for float32 queries too (4e-4).
  *
  * pq_shared_attention: the last n_q positions of every sequence attend to the shared prefix and, causally, to their own paged
  * window behind it (pq_window_attention): one softmax over both.  q_dev, out_dev [batch][n_q][n_q_heads][head_dim].  The

@@ -1035,13 +1035,13 @@ static int32_t launch_attention(int32_t head_dim, int32_t n_q_heads, int32_t n_k
     const bool forced = n_q * g <= 32 && pq::take_debug_wait_failure(5), fail_wait = n_q * g <= 32 && pq::take_debug_wait_failure(2);
     pq::AttentionKernel kernel = plan.kernel;
     if ((forced || fail_wait) && kernel == pq::kClusterKernel) kernel = plan.persistent;
-        if (kernel == pq::kTensorKernel && shared != nullptr)
+    if (kernel == pq::kTensorKernel && shared != nullptr)
       return pq::launch_prefix_tc(a, *shared, pq::prefix_tc_splits(n_q, n_kv_heads, g, max_len, n_sm), st);
     if (kernel == pq::kTensorKernel) return pq::launch_prefill_tc(a, batch, n_q, plan.n_splits, st);
     a.debug = fail_wait ? 1u : 0u;
     if (shared != nullptr && shared->window != nullptr) {
       // the window's blocks first: the cluster and the persistent kernel start beside them (12/12 heads, four queries over 362 compressed and
-      // 1548 recent tokens 24 -> 16 us; two over 25542 and 1647, 16/2 heads, 48 -> 46)
+      // 1548 recent tokens 24 -> 16 us; two over 25542 and 1647, 16/2 heads, 48 -> 46).  The rows kernel, between two kernels of its own, does not
       const int32_t first = pq::launch_window_call(*shared->window, false, st);
       if (first != PQ_OK) return first;
       a.early = c.early = 1;

@@ -13,7 +13,7 @@
 // Bound by instruction issue and the latency of the lookups: 0.93 us per block of a pair at first (prefill_tc_kernel 1.0) with 4900 warp
 // instructions per CTA, now about 4000; then, without the lookups 0.84, without the exponentials 0.82, without both 0.69, and with a third of the
 // score MMAs as well 0.62.  A CTA alone with 128 rows, whole blocks and two stages takes 1.5 us a block and is faster nowhere.  Measured with the
-// rotations, 32/8 heads: 64 queries over 32768 tokens 74 to 76 us (90 in prefill_tc_kernel); the kernel alone 71 with caches cold, its MMAs 56 % of that.
+// rotations, 32/8 heads: 64 queries over 32768 tokens 75 us (90 in prefill_tc_kernel); the kernel alone 71 with caches cold, its MMAs 56 % of that.
 #pragma once
 
 #include "pq_tc_common.cuh"

@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(128) advance_windows_kernel(const __grid_const
 // The rows as 16-byte pieces, where they lie on 16 bytes and the rotated part of a head is a multiple of 32.  An item is two pieces of
 // one head of one row: the two sides of kV rotated pairs, or copied elements.  A block takes kApItems items per thread of a few
 // rows -- all loads go out before anything else --, looks up where its rows go, forms the cosines and sines of each row once for
-// all heads, and stores.  Bound by HBM: 43456 rows of 32/8 heads of 128 in bf16 (1.07 GB in and out) 193 us, 5.5 TB/s; a thread per pair with
+// all heads, and stores.  Bound by HBM: 43456 rows of 32/8 heads of 128 in bf16 (1.07 GB in and out) 192 to 205 us, 5.2 to 5.6 TB/s; a thread per pair with
 // its own cosine and sine took 1554.
 constexpr int kApThreads = 256, kApItems = 3, kApTokens = 8, kApMaxHalf = 64;
 template <class T>

@@ -307,7 +307,7 @@ static WindowRows window_rows_of_lanes(int d, int kv_dtype, int64_t all) {
 }
 // On tensor cores 16 rows and four streams are as fast as 64 and one (the blocks that share a window's tokens find them in L2), or faster where
 // that leaves no rows empty and needs no parts: 35 rows over 2048 tokens 23.0 and 24.5 us (clusters of four), 32 over 2000 15.3 and 17.3 (32 rows and two
-// streams), 64 over 4000 25.4 and 31.6, 64 over 2048 of 32 sequences 132 both.  With more than 48 rows over windows larger than L2 one
+// streams), 64 over 4000 25.4 and 31.6, 64 over 2048 of 32 sequences 132 both.  With more than 48 rows over windows larger than L2 (126 MB) one
 // reading is: eight sequences of 8192 138 and 115.
 static WindowRows window_rows(int d, int kv_dtype, int batch, int n_q, int n_kv_heads, int g, int max_len) {
   const int64_t all = (int64_t)n_q * g;
