@@ -3,10 +3,11 @@ import numpy as np
 import pytest
 import torch
 
+import paper_2502_02617_b200 as pq
 from paper_2502_02617_b200 import synthetic
 from parity_utils import to_f64
 from test_gpu_shared_prefix import check, decoded, make_cache, reference
-from test_gpu_window import BF16, DEV, F32, f64, fill_windows, half_step, make_window
+from test_gpu_window import BF16, DEV, F32, check_append, f64, fill_windows, half_step, make_window
 from window_reference import attention, rows_of
 
 pytestmark = pytest.mark.gpu
@@ -44,3 +45,22 @@ def test_as_many_queries_as_are_allowed(d, hq, hkv, n_queries):
     want, _ = reference(to_f64(few), K, V, d ** -0.5)
     check(cache, few, out[:some], want)
     assert torch.equal(out, out[:some].repeat(-(-n_queries // some), 1, 1)[:n_queries])
+
+
+@pytest.mark.parametrize("kind", ["one", "ragged"])
+@pytest.mark.parametrize("hq,hkv,d,dtype", [(64, 8, 128, F32), (96, 24, 128, BF16), (300, 1, 64, BF16)])
+def test_appended_rows_of_more_pieces_than_a_block_takes(hq, hkv, d, dtype, kind):
+    """A row's 16-byte pieces go to several blocks."""
+    assert (hq + 2 * hkv) * d * (4 if dtype == F32 else 2) // 32 > 768
+    before, counts = [0, 5, 31], [1, 1, 1] if kind == "one" else [20, 0, 7]
+    w = make_window(3, hq, hkv, d, 16, 40, dtype, seed=2, frequencies=pq.pq_rotary_frequencies(d))
+    w.lens.copy_(torch.tensor(before, dtype=torch.int32))
+    g = torch.Generator(DEV).manual_seed(3)
+    q, k, v = (torch.randn((sum(counts), h, d), generator=g, device=DEV).to(dtype) for h in (hq, hkv, hkv))
+    cu = None if kind == "one" else torch.tensor(np.concatenate(([0], np.cumsum(counts))), dtype=torch.int32, device=DEV)
+    pool = f64(w.pool)
+    got = w.append(q, k, v, cu)
+    torch.cuda.synchronize()
+    assert w.check_status()[0] == 0
+    want = check_append(w, counts, q, k, v, cu, None, pool, before)
+    assert np.all(np.abs(f64(got) - want) <= 2.0 ** -18 * 5 + half_step(dtype) * np.abs(want))
